@@ -383,6 +383,67 @@ lomo_status lomo_cross_entropy(const lomo_half* logits, const int32_t* targets, 
 lomo_status lomo_cross_entropy_mean(const lomo_half* logits, const int32_t* targets, double loss_scale, float* loss,
                                     lomo_half* dlogits, double* stats, int64_t T, int64_t V, void* stream);
 
+/* ---------------------------------------------------------------- students and long packed sequences
+ * Steps that take the place of lomo_rope_forward, lomo_attention_forward / _backward and lomo_cross_entropy(_mean) where a
+ * model is fine-tuned on sequences of any length packed into one batch, with pictures or video among the tokens, with heads that share
+ * keys and values, with attention that reaches a limited distance, or from a teacher.  Same storage convention (fp16 tensors, fp32
+ * arithmetic, one rounding per stored element). */
+
+/* Rotary position step with several axes (time, height, width ...).  x [T x ldx], y [T x ldy], of whose rows the first n_heads *
+ * head_dim elements are heads to be turned (and the only ones that are read or written; ldx, ldy >= n_heads * head_dim, multiples of 8):
+ *   y_c = x_c cos - x_{c + head_dim/2} sin,  y_{c + head_dim/2} = x_{c + head_dim/2} cos + x_c sin,
+ * cos, sin = rope_cos, rope_sin [n_positions x head_dim/2] (fp32) at row positions[pair_axis[c] * T + t], column c.
+ * positions: device int32 [n_axes x T]; a position outside [0, n_positions) leaves the pair as it is.  pair_axis: HOST array of
+ * head_dim/2 bytes, each below n_axes, read during the call: sections of pairs, interleaved axes, any assignment.
+ * inverse != 0 turns by the negative angles: the gradient's step.  y may be x itself (with ldy = ldx), otherwise they may not overlap.
+ * head_dim % 16 == 0 and at most 256; 1 <= n_axes <= 8. */
+lomo_status lomo_rope_axes(const lomo_half* x, int64_t ldx, lomo_half* y, int64_t ldy, const float* rope_cos, const float* rope_sin,
+                           int64_t n_positions, const int32_t* positions, int64_t n_axes, const uint8_t* pair_axis,
+                           int64_t T, int64_t n_heads, int64_t head_dim, int inverse, void* stream);
+
+/* Softmax attention over packed sequences with a sliding window and sinks.  Sequence b has the rows seq_offsets[b] ..
+ * seq_offsets[b + 1) - 1 (device int32 [B + 1], ascending within [0, T]; a sequence may be empty; offsets that break this are
+ * clamped: results are then undefined, accesses stay in bounds).  Query i of a sequence sees the keys j <= i with i - j < window or
+ * j < sinks; window >= 1, 0 <= sinks <= 64; a window of T or more is plain causal attention.
+ *   qkv  [T x (n_heads + 2 n_kv_heads) head_dim]: rotated q | rotated k | v; query head n reads key head n / (n_heads / n_kv_heads)
+ *   o    [T x n_heads * head_dim],  lse [T x n_heads] fp32: log sum_j exp(q_i . k_j / sqrt(head_dim)) over the keys seen
+ * Rows that belong to no sequence are neither read nor written.  head_dim is 64 or 128, n_heads a multiple of n_kv_heads.
+ * Probabilities pass through fp16 before they multiply v; o is rounded once.  Deterministic, and a sequence's results do not depend on
+ * the others.  What the mask hides from a query does not reach it, be it inf or NaN. */
+lomo_status lomo_window_attention_forward(const lomo_half* qkv, lomo_half* o, float* lse, const int32_t* seq_offsets, int64_t T, int64_t B,
+                                          int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, int64_t window, int64_t sinks,
+                                          void* stream);
+
+/* Its gradient: dqkv [T x (n_heads + 2 n_kv_heads) head_dim] out: dq | dk | dv with respect to the rotated q, rotated k and v
+ * (lomo_rope_axes with `inverse` on the heads of dq and dk follows).  o, lse: what the forward left; dO [T x n_heads * head_dim].
+ * dk and dv of a key head are sums over its query heads, in fp32.  P and dS pass through fp16 before the products that consume them.
+ * Rows that belong to no sequence are left as they are.  ws: device workspace, 16-byte aligned, of at least
+ * lomo_window_attention_workspace_bytes(...) bytes (do . o of every row and head, and partial sums of the sinks' gradients, whose queries
+ * are the whole sequence); no need to clear it.  Deterministic (no atomics). */
+lomo_status lomo_window_attention_backward(const lomo_half* qkv, const lomo_half* o, const lomo_half* dO, const float* lse, lomo_half* dqkv,
+                                           const int32_t* seq_offsets, int64_t T, int64_t B, int64_t n_heads, int64_t n_kv_heads,
+                                           int64_t head_dim, int64_t window, int64_t sinks, void* ws, size_t ws_bytes, void* stream);
+/* 0 for T == 0, B == 0 or sizes that the calls refuse (host function). */
+size_t lomo_window_attention_workspace_bytes(int64_t T, int64_t B, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, int64_t sinks);
+
+/* Token losses and their scaled gradient for a student with logits z [T x V] whose teacher is known by K top logits a token
+ * (teacher_ids int32 [T x K], teacher_logits [T x K]), at a temperature tau > 0, with weight w = soft_weight in [0, 1]:
+ *   p = softmax(teacher_logits / tau) over the listed ones,  q = softmax(z / tau),
+ *   loss = (1 - w) (lse(z) - z[target]) + w tau^2 sum_k p_k (log p_k - log q[id_k]),
+ *   dlogits_j = grad_scale * ((1 - w) (softmax(z)_j - [j = target]) + w tau (q_j - sum of p_k with id_k = j)).
+ * An id outside [0, V) or a teacher logit of -inf is not listed; an id listed twice has both its shares; a token with nothing listed
+ * has the first term alone.  targets [T] int32: a target outside [0, V) leaves its token out (loss 0, zero gradient row), also where
+ * w = 1.  1 <= K <= 1024, V % 8 == 0.  loss [T] fp32.  dlogits may be the logits buffer itself.  Deterministic. */
+lomo_status lomo_distill(const lomo_half* logits, const int32_t* teacher_ids, const lomo_half* teacher_logits, const int32_t* targets,
+                         float grad_scale, float temperature, float soft_weight, float* loss, lomo_half* dlogits,
+                         int64_t T, int64_t V, int64_t K, void* stream);
+
+/* The mean loss of a batch in one call, as lomo_cross_entropy_mean: n counted targets, grad_scale = (float)(loss_scale / n),
+ * stats[0] = sum_t loss[t] / n and stats[1] = n (device double[3]; stats[2] is scratch). */
+lomo_status lomo_distill_mean(const lomo_half* logits, const int32_t* teacher_ids, const lomo_half* teacher_logits, const int32_t* targets,
+                              double loss_scale, float temperature, float soft_weight, float* loss, lomo_half* dlogits, double* stats,
+                              int64_t T, int64_t V, int64_t K, void* stream);
+
 /* Kernel families for lomo_timing_read. */
 enum { LOMO_KERNEL_WGRAD_UPDATE = 0, LOMO_KERNEL_WGRAD_SQNORM = 1, LOMO_KERNEL_DGRAD = 2,
        LOMO_KERNEL_EMBEDDING = 3, LOMO_KERNEL_VECTOR = 4, LOMO_KERNEL_GRAM_SQNORM = 5, LOMO_KERNEL_CHAIN = 6,

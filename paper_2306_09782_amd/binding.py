@@ -25,6 +25,8 @@ EXPORTED_SYMBOLS = (
     "lomo_cross_entropy", "lomo_embedding_forward", "lomo_linear_forward_residual", "lomo_cross_entropy_mean",
     "lomo_probe_mfma", "lomo_probe_copy", "lomo_vector_update_static", "lomo_contraction_tiles",
     "lomo_contraction_plan",
+    "lomo_rope_axes", "lomo_window_attention_forward", "lomo_window_attention_backward", "lomo_window_attention_workspace_bytes",
+    "lomo_distill", "lomo_distill_mean",
 )
 
 
@@ -106,6 +108,12 @@ def load_library():
         "lomo_probe_copy": (c_int, [P, P, c_size_t, P]),
         "lomo_contraction_tiles": (c_int, [c_int, POINTER(c_int64), I64, POINTER(c_int32)]),
         "lomo_contraction_plan": (c_int, [c_int, c_int, POINTER(c_int64), I64, POINTER(c_int32), POINTER(c_int32)]),
+        "lomo_rope_axes": (c_int, [P, I64, P, I64, P, P, I64, P, I64, c_char_p, I64, I64, I64, c_int, P]),
+        "lomo_window_attention_forward": (c_int, [P, P, P, P, I64, I64, I64, I64, I64, I64, I64, P]),
+        "lomo_window_attention_backward": (c_int, [P, P, P, P, P, P, I64, I64, I64, I64, I64, I64, I64, P, c_size_t, P]),
+        "lomo_window_attention_workspace_bytes": (c_size_t, [I64, I64, I64, I64, I64, I64]),
+        "lomo_distill": (c_int, [P, P, P, P, c_float, c_float, c_float, P, P, I64, I64, I64, P]),
+        "lomo_distill_mean": (c_int, [P, P, P, P, c_double, c_float, c_float, P, P, P, I64, I64, I64, P]),
         "lomo_timing_enable": (c_int, [c_int]),
         "lomo_timing_read": (c_int, [c_int, POINTER(c_double), POINTER(c_int64)]),
     }
@@ -397,6 +405,113 @@ def lomo_cross_entropy_mean(logits, targets, loss_scale, loss, dlogits, stats, s
     assert targets.numel() == T and loss.numel() == T and tuple(dlogits.shape) == (T, V) and _nbytes(stats) >= 24
     _check(load_library().lomo_cross_entropy_mean(_ptr(logits), _ptr(targets), loss_scale, _ptr(loss), _ptr(dlogits),
                                                   _ptr(stats), T, V, _stream(stream)))
+
+
+def _expect(t, dtype, shape, name, device=None):
+    """`t` as the C side takes it for granted: its type, its shape (None: any size), dense rows, its device."""
+    if t.dtype != dtype or t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
+        raise LomoError(f"{name}: {str(t.dtype)[6:]} {tuple(t.shape)}, want {str(dtype)[6:]} {shape}")
+    if not t.is_contiguous():
+        raise LomoError(f"{name} is not contiguous")
+    _on_device(t, name, device)
+
+
+def _on_device(t, name, device):
+    if device is not None and t.device != device:
+        raise LomoError(f"{name} is on {t.device}, not on {device}")
+
+
+def _current_device(t, name):
+    """The tensors' common device, which has to be the current one: that is where the launches go."""
+    import torch
+    if t.device.type != "cuda" or t.device.index != torch._C._cuda_getDevice():
+        raise LomoError(f"{name} is on {t.device}, which is not the current device")
+    return t.device
+
+
+def lomo_rope_axes(x, y, rope_cos, rope_sin, positions, pair_axis, n_heads, head_dim, inverse=False, stream=None):
+    """Rows of x and y may be longer than n_heads * head_dim and need not be adjacent; y may be x.  positions [axes x T];
+    pair_axis: the axis of each of the head_dim / 2 pairs (a sequence of int)."""
+    import torch
+    T, device = x.shape[0], _current_device(x, "x")
+    for t, name in ((x, "x"), (y, "y")):
+        if t.dtype != torch.float16 or t.dim() != 2 or t.shape[0] != T or t.shape[1] < n_heads * head_dim or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise LomoError(f"{name}: {str(t.dtype)[6:]} {tuple(t.shape)}, want float16 [{T} x at least {n_heads * head_dim}] with dense rows")
+    _on_device(y, "y", device)
+    _expect(rope_cos, torch.float32, (None, head_dim // 2), "rope_cos", device)
+    _expect(rope_sin, torch.float32, tuple(rope_cos.shape), "rope_sin", device)
+    _expect(positions, torch.int32, (None, T), "positions", device)
+    axes = bytes(pair_axis)
+    if len(axes) != head_dim // 2:
+        raise LomoError(f"pair_axis has {len(axes)} entries, want {head_dim // 2}")
+    ld = lambda t: t.stride(0) if T > 1 else max(t.shape[1] // 8 * 8, n_heads * head_dim)      # torch gives a single row any stride
+    _check(load_library().lomo_rope_axes(_ptr(x), ld(x), _ptr(y), ld(y), _ptr(rope_cos), _ptr(rope_sin), rope_cos.shape[0], _ptr(positions),
+                                         positions.shape[0], axes, T, n_heads, head_dim, 1 if inverse else 0, _stream(stream)))
+
+
+def _window_sizes(qkv, o, lse, seq_offsets, n_heads, n_kv_heads):
+    import torch
+    T, device = qkv.shape[0], _current_device(qkv, "qkv")
+    if n_heads < 1 or n_kv_heads < 1 or o.dim() != 2 or o.shape[1] % n_heads:
+        raise LomoError(f"o: {tuple(o.shape)} for {n_heads} heads, {n_kv_heads} of keys")
+    d = o.shape[1] // n_heads
+    _expect(qkv, torch.float16, (T, (n_heads + 2 * n_kv_heads) * d), "qkv", device)
+    _expect(o, torch.float16, (T, n_heads * d), "o", device)
+    _expect(lse, torch.float32, (T, n_heads), "lse", device)
+    _expect(seq_offsets, torch.int32, (None,), "seq_offsets", device)
+    if seq_offsets.numel() < 1:
+        raise LomoError("seq_offsets is empty")
+    return T, seq_offsets.numel() - 1, d, device
+
+
+def lomo_window_attention_forward(qkv, o, lse, seq_offsets, n_heads, n_kv_heads, window, sinks=0, stream=None):
+    """seq_offsets: int32 [number of sequences + 1] on the device."""
+    T, B, d, _ = _window_sizes(qkv, o, lse, seq_offsets, n_heads, n_kv_heads)
+    _check(load_library().lomo_window_attention_forward(_ptr(qkv), _ptr(o), _ptr(lse), _ptr(seq_offsets), T, B, n_heads, n_kv_heads, d,
+                                                        window, sinks, _stream(stream)))
+
+
+def lomo_window_attention_workspace_bytes(T: int, B: int, n_heads: int, n_kv_heads: int, head_dim: int, sinks: int = 0) -> int:
+    return load_library().lomo_window_attention_workspace_bytes(T, B, n_heads, n_kv_heads, head_dim, sinks)
+
+
+def lomo_window_attention_backward(qkv, o, dO, lse, dqkv, seq_offsets, n_heads, n_kv_heads, window, sinks, ws, stream=None):
+    import torch
+    T, B, d, device = _window_sizes(qkv, o, lse, seq_offsets, n_heads, n_kv_heads)
+    _expect(dO, torch.float16, tuple(o.shape), "dO", device)
+    _expect(dqkv, torch.float16, tuple(qkv.shape), "dqkv", device)
+    _on_device(ws, "ws", device)
+    _check(load_library().lomo_window_attention_backward(_ptr(qkv), _ptr(o), _ptr(dO), _ptr(lse), _ptr(dqkv), _ptr(seq_offsets), T, B,
+                                                         n_heads, n_kv_heads, d, window, sinks, _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def _distill_sizes(logits, teacher_ids, teacher_logits, targets, loss, dlogits):
+    import torch
+    device = _current_device(logits, "logits")
+    _expect(logits, torch.float16, (None, None), "logits")
+    T, V = logits.shape
+    _expect(teacher_ids, torch.int32, (T, None), "teacher_ids", device)
+    K = teacher_ids.shape[1]
+    _expect(teacher_logits, torch.float16, (T, K), "teacher_logits", device)
+    _expect(targets, torch.int32, (T,), "targets", device)
+    _expect(loss, torch.float32, (T,), "loss", device)
+    _expect(dlogits, torch.float16, (T, V), "dlogits", device)
+    return T, V, K, device
+
+
+def lomo_distill(logits, teacher_ids, teacher_logits, targets, grad_scale, temperature, soft_weight, loss, dlogits, stream=None):
+    T, V, K, _ = _distill_sizes(logits, teacher_ids, teacher_logits, targets, loss, dlogits)
+    _check(load_library().lomo_distill(_ptr(logits), _ptr(teacher_ids), _ptr(teacher_logits), _ptr(targets), grad_scale, temperature,
+                                       soft_weight, _ptr(loss), _ptr(dlogits), T, V, K, _stream(stream)))
+
+
+def lomo_distill_mean(logits, teacher_ids, teacher_logits, targets, loss_scale, temperature, soft_weight, loss, dlogits, stats, stream=None):
+    """stats: device float64[3]; receives (mean loss over the counted targets, their number, scratch)."""
+    import torch
+    T, V, K, device = _distill_sizes(logits, teacher_ids, teacher_logits, targets, loss, dlogits)
+    _expect(stats, torch.float64, (3,), "stats", device)
+    _check(load_library().lomo_distill_mean(_ptr(logits), _ptr(teacher_ids), _ptr(teacher_logits), _ptr(targets), loss_scale, temperature,
+                                            soft_weight, _ptr(loss), _ptr(dlogits), _ptr(stats), T, V, K, _stream(stream)))
 
 
 PROBE_OPERAND_BYTES = 16 * 64 * 16

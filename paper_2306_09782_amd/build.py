@@ -21,8 +21,8 @@ LIB_DIR = os.path.join(HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "liblomo.so")
 OBJ_DIR = os.path.join(ROOT, "_build", "lomo")
 SOURCES = ["lomo_api.hip", "lomo_gemm.hip", "lomo_gemm_dma.hip", "lomo_gemm_wide.hip", "lomo_gemm_tile.hip", "lomo_gram.hip", "lomo_chain.hip",
-           "lomo_attention.hip", "lomo_attention_fwd.hip", "lomo_forward.hip", "lomo_rowops.hip", "lomo_timing.hip",
-           "lomo_ceiling.hip", "lomo_static.hip"]
+           "lomo_attention.hip", "lomo_attention_fwd.hip", "lomo_forward.hip", "lomo_window.hip", "lomo_window_fwd.hip", "lomo_rope_axes.hip",
+           "lomo_distill.hip", "lomo_rowops.hip", "lomo_timing.hip", "lomo_ceiling.hip", "lomo_static.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU arithmetic is kept off on the test machines.  -Xclang reaches both passes of a HIP

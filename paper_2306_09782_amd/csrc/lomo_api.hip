@@ -14,6 +14,14 @@ namespace {
 
 inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 inline lomo_status from_hip(hipError_t e) { return e == hipSuccess ? LOMO_OK : LOMO_ERR_LAUNCH; }
+inline bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+
+// What the calls on packed sequences ask of their sizes.
+inline bool window_sizes_ok(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks) {
+    if (T < 0 || B < 0 || h <= 0 || g <= 0 || h % g != 0 || (d != 64 && d != 128) || sinks < 0 || sinks > 64) return false;
+    if (T > (1 << 30) || B > (1 << 24) || h > (1 << 16)) return false;      // with this, 64 rows stay below 4 GiB
+    return window_attention_pieces(T, B) * h <= 0x7fffffff;
+}
 inline float step_size(float lr, float inv_loss_scale, float clip_coef) {
     return (float)((double)lr * (double)clip_coef * (double)inv_loss_scale);
 }
@@ -686,6 +694,105 @@ lomo_status lomo_attention_backward(const lomo_half* qkv, const lomo_half* o, co
     hipStream_t st = static_cast<hipStream_t>(stream);
     ScopedTiming timing(LOMO_KERNEL_ATTENTION, st);
     return from_hip(launch_attention_backward(qkv, o, dO, lse, rope_cos, rope_sin, delta_ws, dqkv, B, s, n_heads, st));
+}
+
+lomo_status lomo_rope_axes(const lomo_half* x, int64_t ldx, lomo_half* y, int64_t ldy, const float* rope_cos, const float* rope_sin,
+                           int64_t n_positions, const int32_t* positions, int64_t n_axes, const uint8_t* pair_axis, int64_t T,
+                           int64_t n_heads, int64_t head_dim, int inverse, void* stream) {
+    if (T < 0 || n_positions < 0 || n_axes < 1 || n_axes > 8 || n_heads < 0 || head_dim < 16 || head_dim > 256 || (head_dim & 15))
+        return LOMO_ERR_SHAPE;
+    if (T > 0x7fffffff || n_heads > (1 << 16) || (ldx & 7) || (ldy & 7) || ldx < n_heads * head_dim || ldy < n_heads * head_dim || (x == y && ldx != ldy))
+        return LOMO_ERR_SHAPE;
+    if (!pair_axis) return LOMO_ERR_NULL;
+    for (int64_t c = 0; c < head_dim / 2; ++c)
+        if (pair_axis[c] >= n_axes) return LOMO_ERR_SHAPE;
+    if (T == 0 || n_heads == 0) return LOMO_OK;
+    if (!x || !y || !positions || (n_positions > 0 && (!rope_cos || !rope_sin))) return LOMO_ERR_NULL;
+    if (misaligned(x) || misaligned(y) || misaligned4(rope_cos) || misaligned4(rope_sin) || misaligned4(positions)) return LOMO_ERR_ALIGN;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ScopedTiming timing(LOMO_KERNEL_CHAIN, st);
+    return from_hip(launch_rope_axes(x, ldx, y, ldy, rope_cos, rope_sin, n_positions, positions, pair_axis, T, n_heads, head_dim,
+                                     inverse != 0, st));
+}
+
+size_t lomo_window_attention_workspace_bytes(int64_t T, int64_t B, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, int64_t sinks) {
+    if (!window_sizes_ok(T, B, n_heads, n_kv_heads, head_dim, sinks) || T == 0 || B == 0) return 0;
+    return window_attention_ws_bytes(T, B, n_heads, n_kv_heads, head_dim, sinks);
+}
+
+lomo_status lomo_window_attention_forward(const lomo_half* qkv, lomo_half* o, float* lse, const int32_t* seq_offsets, int64_t T, int64_t B,
+                                          int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, int64_t window, int64_t sinks,
+                                          void* stream) {
+    if (!window_sizes_ok(T, B, n_heads, n_kv_heads, head_dim, sinks) || window < 1) return LOMO_ERR_SHAPE;
+    if (T == 0 || B == 0) return LOMO_OK;
+    if (!qkv || !o || !lse || !seq_offsets) return LOMO_ERR_NULL;
+    if (misaligned(qkv) || misaligned(o) || misaligned4(lse) || misaligned4(seq_offsets)) return LOMO_ERR_ALIGN;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ScopedTiming timing(LOMO_KERNEL_ATTENTION, st);
+    return from_hip(launch_window_attention_forward(qkv, o, lse, seq_offsets, T, B, n_heads, n_kv_heads, head_dim, window < T ? window : T,
+                                                    sinks, st));
+}
+
+lomo_status lomo_window_attention_backward(const lomo_half* qkv, const lomo_half* o, const lomo_half* dO, const float* lse, lomo_half* dqkv,
+                                           const int32_t* seq_offsets, int64_t T, int64_t B, int64_t n_heads, int64_t n_kv_heads,
+                                           int64_t head_dim, int64_t window, int64_t sinks, void* ws, size_t ws_bytes, void* stream) {
+    if (!window_sizes_ok(T, B, n_heads, n_kv_heads, head_dim, sinks) || window < 1) return LOMO_ERR_SHAPE;
+    if (T == 0 || B == 0) return LOMO_OK;
+    if (!qkv || !o || !dO || !lse || !dqkv || !seq_offsets) return LOMO_ERR_NULL;
+    if (misaligned(qkv) || misaligned(o) || misaligned(dO) || misaligned4(lse) || misaligned(dqkv) || misaligned4(seq_offsets) || misaligned(ws))
+        return LOMO_ERR_ALIGN;
+    if (!ws || ws_bytes < window_attention_ws_bytes(T, B, n_heads, n_kv_heads, head_dim, sinks)) return LOMO_ERR_WORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ScopedTiming timing(LOMO_KERNEL_ATTENTION, st);
+    return from_hip(launch_window_attention_backward(qkv, o, dO, lse, dqkv, seq_offsets, T, B, n_heads, n_kv_heads, head_dim,
+                                                     window < T ? window : T, sinks, ws, st));
+}
+
+}  // extern "C"
+
+// What lomo_distill and lomo_distill_mean ask of what they share.
+static lomo_status distill_arguments(const lomo_half* logits, const int32_t* ids, const lomo_half* teacher, const int32_t* targets,
+                                     float temperature, float soft_weight, float* loss, lomo_half* dlogits, int64_t T, int64_t V, int64_t K) {
+    if (T < 0 || V < 0 || (V & 7) || T > 0x7fffffff || V > 0x7fffffff || K < 1 || K > 1024) return LOMO_ERR_SHAPE;
+    if (!(temperature > 0.f) || !isfinite(temperature) || !(soft_weight >= 0.f && soft_weight <= 1.f)) return LOMO_ERR_SHAPE;
+    if (T == 0) return LOMO_OK;
+    if (V == 0) return LOMO_ERR_SHAPE;
+    if (!logits || !ids || !teacher || !targets || !loss || !dlogits) return LOMO_ERR_NULL;
+    if (misaligned(logits) || misaligned(dlogits) || misaligned4(ids) || (reinterpret_cast<uintptr_t>(teacher) & 1u) || misaligned4(targets) ||
+        misaligned4(loss))
+        return LOMO_ERR_ALIGN;
+    return LOMO_OK;
+}
+
+extern "C" {
+
+lomo_status lomo_distill(const lomo_half* logits, const int32_t* teacher_ids, const lomo_half* teacher_logits, const int32_t* targets,
+                         float grad_scale, float temperature, float soft_weight, float* loss, lomo_half* dlogits, int64_t T, int64_t V,
+                         int64_t K, void* stream) {
+    const lomo_status bad = distill_arguments(logits, teacher_ids, teacher_logits, targets, temperature, soft_weight, loss, dlogits, T, V, K);
+    if (bad != LOMO_OK || T == 0) return bad;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ScopedTiming timing(LOMO_KERNEL_CHAIN, st);
+    return from_hip(launch_distill(logits, teacher_ids, teacher_logits, targets, grad_scale, nullptr, temperature, soft_weight, loss, dlogits,
+                                   T, V, K, st));
+}
+
+lomo_status lomo_distill_mean(const lomo_half* logits, const int32_t* teacher_ids, const lomo_half* teacher_logits, const int32_t* targets,
+                              double loss_scale, float temperature, float soft_weight, float* loss, lomo_half* dlogits, double* stats,
+                              int64_t T, int64_t V, int64_t K, void* stream) {
+    if (!(loss_scale > 0.0)) return LOMO_ERR_SHAPE;
+    const lomo_status bad = distill_arguments(logits, teacher_ids, teacher_logits, targets, temperature, soft_weight, loss, dlogits, T, V, K);
+    if (bad != LOMO_OK) return bad;
+    if (!stats) return LOMO_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(stats) & 7u) return LOMO_ERR_ALIGN;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ScopedTiming timing(LOMO_KERNEL_CHAIN, st);
+    hipError_t e = launch_count_targets(targets, T, V, loss_scale, stats, st);
+    if (e == hipSuccess && T > 0)
+        e = launch_distill(logits, teacher_ids, teacher_logits, targets, 0.f, reinterpret_cast<const float*>(stats + 2), temperature, soft_weight,
+                           loss, dlogits, T, V, K, st);
+    if (e == hipSuccess) e = launch_mean_loss(loss, T, stats, st);
+    return from_hip(e);
 }
 
 lomo_status lomo_reduce_flags(const int32_t* flags, int64_t n, int32_t* out, void* stream) {

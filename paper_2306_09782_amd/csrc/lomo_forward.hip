@@ -232,6 +232,15 @@ __global__ __launch_bounds__(FW_NT) void mean_loss_kernel(const float* __restric
     if (threadIdx.x == 0) stats[0] = stats[1] > 0.0 ? red[0] / stats[1] : 0.0;
 }
 
+hipError_t launch_count_targets(const int32_t* target, int64_t T, int64_t V, double loss_scale, double* stats, hipStream_t st) {
+    hipLaunchKernelGGL(count_targets_kernel, dim3(1), dim3(FW_NT), 0, st, target, T, V, loss_scale, stats);
+    return hipGetLastError();
+}
+hipError_t launch_mean_loss(const float* loss, int64_t T, double* stats, hipStream_t st) {
+    hipLaunchKernelGGL(mean_loss_kernel, dim3(1), dim3(FW_NT), 0, st, loss, T, stats);
+    return hipGetLastError();
+}
+
 // stats: device double[3]; [0] mean loss, [1] counted targets, [2] scratch (the gradient scale as a float).
 hipError_t launch_cross_entropy_mean(const uint16_t* z, const int32_t* target, double loss_scale, float* loss, uint16_t* dz,
                                      double* stats, int64_t T, int64_t V, hipStream_t st) {

@@ -213,6 +213,22 @@ hipError_t launch_attention_backward(const uint16_t* qkv, const uint16_t* o, con
                                      const float* cosv, const float* sinv, float* delta, uint16_t* dqkv, int64_t B, int64_t s,
                                      int64_t nh, hipStream_t st);
 
+// Operators for students and long packed sequences (lomo_rope_axes.hip, lomo_window_fwd.hip, lomo_window.hip, lomo_distill.hip).
+hipError_t launch_rope_axes(const uint16_t* x, int64_t ldx, uint16_t* y, int64_t ldy, const float* cosv, const float* sinv, int64_t P,
+                            const int32_t* pos, const uint8_t* axis, int64_t T, int64_t heads, int64_t d, bool inverse, hipStream_t st);
+int64_t window_attention_pieces(int64_t T, int64_t B);      // workgroups of a call for each head
+size_t window_attention_ws_bytes(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks);
+hipError_t launch_window_attention_forward(const uint16_t* qkv, uint16_t* o, float* lse, const int32_t* off, int64_t T, int64_t B, int64_t h,
+                                           int64_t g, int64_t d, int64_t window, int64_t sinks, hipStream_t st);
+hipError_t launch_window_attention_backward(const uint16_t* qkv, const uint16_t* o, const uint16_t* dO, const float* lse, uint16_t* dqkv,
+                                            const int32_t* off, int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t window,
+                                            int64_t sinks, void* ws, hipStream_t st);
+hipError_t launch_distill(const uint16_t* z, const int32_t* ids, const uint16_t* teacher, const int32_t* target, float scale,
+                          const float* scale_dev, float tau, float w, float* loss, uint16_t* dz, int64_t T, int64_t V, int64_t K,
+                          hipStream_t st);
+hipError_t launch_count_targets(const int32_t* target, int64_t T, int64_t V, double loss_scale, double* stats, hipStream_t st);
+hipError_t launch_mean_loss(const float* loss, int64_t T, double* stats, hipStream_t st);
+
 hipError_t launch_reduce_flags(const int32_t* flags, int64_t n, int32_t* out, hipStream_t st);
 
 }  // namespace lomo

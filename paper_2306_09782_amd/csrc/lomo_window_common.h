@@ -1,0 +1,200 @@
+// Pieces shared by the kernels of attention with a sliding window and sinks: which sequence a workgroup's rows belong to, tiles
+// of D = 64 or 128 columns in LDS, their loads, fragment reads, and which pairs a mask leaves.
+//
+// Rows of q, k, v, o are packed: sequence b has the rows off[b] .. off[b + 1) - 1.  Query i of a sequence sees the keys j <= i
+// with i - j < window or j < sinks.  A workgroup of four waves owns 128 rows (queries, or keys), 32 per wave, which stay in
+// registers as MFMA fragments; pairs of [64 x D] tiles move along the sequence, double-buffered in LDS.  Scores are formed
+// so that a lane owns one of the wave's rows; a block of 32 x 32 of them, one lane pair's sixteen registers, is what is masked,
+// skipped or taken whole.
+#pragma once
+#include "lomo_attention_common.h"
+#include "lomo_gemm_dma_common.h"
+
+namespace lomo {
+namespace win {
+
+using attn::fragment_of;
+using attn::pack2;
+using attn::read8;
+using attn::read_tr8;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int ROWS = 128, BLK = 64;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+template <int D>
+constexpr int TILE = BLK * D;      // halves
+template <int D>
+constexpr int PAIR = 2 * TILE<D>;
+template <int D>
+constexpr float SCALE = D == 128 ? 0.08838834764831845f : 0.125f;      // 1 / sqrt(D)
+
+// What the calls have in common.
+struct Batch {
+    const int32_t* off;      // [B + 1]
+    int T, B, h, g;          // rows, sequences, query heads, key heads
+    int window, sinks;
+};
+
+// A sequence's rows; offsets that do not ascend within [0, T] cannot lead outside the buffers.
+struct Rows {
+    int start, len;
+};
+__device__ __forceinline__ int clamped(const Batch& a, int b) { return min(max(a.off[b], 0), a.T); }
+__device__ __forceinline__ Rows rows_of(const Batch& a, int b) {
+    const int s = clamped(a, b), e = clamped(a, b + 1);
+    return {s, max(e - s, 0)};
+}
+
+// Pieces of `unit` rows are numbered through all sequences without a table: those of sequence b begin at
+// floor(off[b] / unit) + more * b, which leaves room for ceil(length / unit) + more - 1 of them.  The sequence that number i falls in, by a
+// 64-way search of the wave, or -1.
+__device__ __forceinline__ int first_piece(const Batch& a, int b, int unit, int more) { return clamped(a, b) / unit + more * b; }
+__device__ __forceinline__ int sequence_of(const Batch& a, int i, int unit, int more) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = a.B;
+    while (true) {
+        const int step = (n + 63) >> 6;
+        const bool in = lane * step < n;
+        const bool at_or_before = in && first_piece(a, lo + (in ? lane * step : 0), unit, more) <= i;
+        const int count = __popcll(__ballot(at_or_before));
+        if (count == 0) return -1;
+        lo += (count - 1) * step;
+        n = min(step, n - (count - 1) * step);
+        if (step == 1) return __builtin_amdgcn_readfirstlane(lo);
+    }
+}
+inline int64_t pieces(int64_t T, int64_t B, int64_t unit, int64_t more) { return T / unit + more * B; }
+
+// Place of this workgroup in an order of `total`, cut into one contiguous run for each XCD (blockIdx % 8), so that neighbours
+// in the order meet in one L2.
+__device__ __forceinline__ int place_of_block(int total) {
+    const int x = (int)(blockIdx.x & 7), local = (int)(blockIdx.x >> 3);
+    const int q = total >> 3, r = total & 7;
+    return x * q + (x < r ? x : r) + local;
+}
+
+// Chunk swizzle of a tile with 16-byte chunks: chunk c of row r sits at c ^ swz(r).  256-byte rows as in lomo_attention_common.h.  128-byte
+// rows: rows r and r + 1 are on different halves of the banks anyway; r and r + 2 are 4 chunks apart (the four rows of a transposing read),
+// the next two bits of r move by 1 .. 3 chunks (sixteen rows read at one column).
+template <int D>
+__device__ __forceinline__ int swz(int r) {
+    if constexpr (D == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+    else return ((r & 2) << 1) | ((r >> 2) & 3);
+}
+
+// Load of a [64 x D] tile whose row 0 is at `base` and of which `rows` (any number) lie in the sequence; the others become zeros: the
+// descriptor ends behind the last one.  Rows are `ld` elements apart, 64 of them less than 4 GiB.
+template <int D>
+struct TileLoad {
+    static constexpr int RPI = 512 / D;              // rows that an instruction of a wave fetches
+    uint32_t voff, ld2;
+    __device__ __forceinline__ TileLoad(int64_t ld) {
+        const int lane = threadIdx.x & 63, rr = lane / (D / 8), c = lane % (D / 8);
+        ld2 = 2u * (uint32_t)ld;
+        voff = (uint32_t)rr * ld2 + (uint32_t)((c ^ swz<D>(rr)) * 16);
+    }
+    template <int WAVES = 4>
+    __device__ __forceinline__ void issue(const uint16_t* base, int rows, uint32_t tile, int wave) const {
+        const uint32_t n = (uint32_t)min(max(rows, 0), BLK);
+        const auto srd = dma::make_srd(base, n == 0 ? 0u : (n - 1) * ld2 + 2u * D);
+        constexpr int PER = BLK / RPI / WAVES;
+        // instruction it fetches rows RPI (PER wave + it) ..; their swizzles differ from those of rows 0 .. in the low two chunk bits
+#pragma unroll
+        for (int it = 0; it < PER; ++it) {
+            const int k = PER * wave + it, r0 = RPI * k;
+            uint32_t v = voff ^ (uint32_t)(((r0 >> 2) & 3) * 16);
+            asm volatile("" : "+v"(v));
+            dma::dma16(v + (uint32_t)r0 * ld2, srd, 0u, tile + (uint32_t)k * 1024u);
+        }
+    }
+};
+
+// Fragment reads from a tile at an LDS address that is a multiple of 256 bytes (see lomo_attention_common.h).
+template <int D>
+struct TileRead {
+    uint32_t row_rd, tr0, tr1;
+    __device__ __forceinline__ TileRead(uint32_t tile) {
+        const int lane = threadIdx.x & 63;
+        const int l32 = lane & 31, lh = lane >> 5;
+        const int g4 = lane >> 4, j16 = lane & 15;
+        const int mhalf = g4 & 1, kh = g4 >> 1, rib = j16 >> 2, piece = j16 & 3;
+        const int tr_row = 8 * kh + rib, tr_col = 16 * mhalf + 4 * piece;
+        row_rd = tile + 2u * (uint32_t)(l32 * D + ((8 * lh) ^ (swz<D>(l32) << 3)));
+        tr0 = tile + 2u * (uint32_t)(tr_row * D + (tr_col ^ (swz<D>(tr_row) << 3)));
+        tr1 = tile + 2u * (uint32_t)((tr_row + 4) * D + (tr_col ^ (swz<D>(tr_row + 4) << 3)));
+    }
+    __device__ __forceinline__ TileRead at(int halves) const {
+        TileRead t = *this;
+        t.row_rd += 2u * (uint32_t)halves;
+        t.tr0 += 2u * (uint32_t)halves;
+        t.tr1 += 2u * (uint32_t)halves;
+        asm volatile("" : "+v"(t.row_rd), "+v"(t.tr0), "+v"(t.tr1));
+        return t;
+    }
+    // rows 0 .. 31, columns 16 ks .. + 15: a lane holds eight consecutive columns of its row
+    __device__ __forceinline__ half8 rows(int off, int ks) const { return read8((row_rd ^ (uint32_t)(32 * ks)) + 2u * (uint32_t)off); }
+    // columns 32 i .. + 31, rows 16 ks .. + 15: a lane holds eight consecutive rows of its column
+    __device__ __forceinline__ half8 columns(int off, int i, int ks) const {
+        const uint32_t o = 2u * (uint32_t)(off + 16 * ks * D);
+        return read_tr8((tr0 ^ (uint32_t)(64 * i)) + o, (tr1 ^ (uint32_t)(64 * i)) + o);
+    }
+};
+
+// This lane's row as fragments: eight consecutive columns each.
+template <int D>
+__device__ __forceinline__ void load_fragments(half8 (&f)[D / 16], const uint16_t* row) {
+    const int lh = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) f[ks] = *reinterpret_cast<const half8*>(row + 16 * ks + 8 * lh);
+}
+
+// acc[i][r]: column 32 i + 8 (r / 4) + 4 lh + r % 4 of the lane's row, rounded once.  Every lane takes part in the exchange; `row` is null for
+// those that have no row.
+template <int N>
+__device__ __forceinline__ void store_rows(const floatx16 (&acc)[N], uint16_t* row) {
+    const int lh = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        uint32_t pk[8];
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) pk[r >> 1] = pack2(acc[i][r], acc[i][r + 1]);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            const half8 f = fragment_of(pk, a);
+            if (row != nullptr) *reinterpret_cast<half8*>(row + 32 * i + 16 * a + 8 * lh) = f;
+        }
+    }
+}
+
+// Whether any of a block's 32 rows [32 x D] in a tile holds inf or NaN.
+template <int D>
+__device__ __forceinline__ bool any_not_finite(const TileRead<D>& r0, int off) {
+    uint32_t worst = 0;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        const u32x4 w = __builtin_bit_cast(u32x4, r0.rows(off, ks));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) worst |= ((w[e] & 0x7c007c00u) + 0x04000400u) & 0x80008000u;      // an exponent of ones carries over
+    }
+    return __any(worst != 0);
+}
+__device__ __forceinline__ half8 finite_or_zero(half8 x) {
+    u32x4 w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t bad = (((w[e] & 0x7c007c00u) + 0x04000400u) & 0x80008000u) >> 15;      // 1 in each half that is not finite
+        w[e] &= ~(bad * 0xffffu);
+    }
+    return __builtin_bit_cast(half8, w);
+}
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+
+// What a mask leaves of queries q0 .. q0 + 31 and keys k0 .. k0 + 31 (uniform in a wave).
+enum Seen { NONE, SOME, ALL };
+__device__ __forceinline__ Seen seen(int q0, int k0, int window, int sinks) {
+    if (k0 > q0 + 31 || (q0 - (k0 + 31) >= window && k0 >= sinks)) return NONE;
+    return k0 + 31 <= q0 && (q0 + 31 - k0 < window || k0 + 31 < sinks) ? ALL : SOME;
+}
+
+}  // namespace win
+}  // namespace lomo
