@@ -16,6 +16,8 @@
 // cuts look for inf and NaN and take them out of the products, so that a pair which the mask hides adds nothing.
 #include "lomo_window_common.h"
 
+#include <type_traits>
+
 namespace lomo {
 
 namespace win {
@@ -82,20 +84,30 @@ __device__ __forceinline__ bool any_not_finite(const floatx16& S, const floatx16
     return __any(bad);
 }
 
-// acc[i] += tile^T[column][row] f[row][lane's row], 32 rows at `off` of the tile; dirty: without what is not finite there.
+// acc[i] += tile^T[column][row] f[row][lane's row], 32 rows at `off` of the tile.
 template <int D>
-__device__ __forceinline__ void multiply(const TileRead<D>& r0, int off, const half8 (&f)[2], floatx16 (&acc)[D / 32], bool dirty) {
-    if (dirty) {
+__device__ __forceinline__ void multiply(const TileRead<D>& r0, int off, const half8 (&f)[2], floatx16 (&acc)[D / 32]) {
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+    for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i)
-                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(finite_or_zero(r0.columns(off, i, ks)), f[ks], acc[i], 0, 0, 0);
-    } else {
+        for (int i = 0; i < D / 32; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.columns(off, i, ks), f[ks], acc[i], 0, 0, 0);
+    attn::interleave<4, 1, 2, D / 16 - 2, 2>();
+    __builtin_amdgcn_sched_barrier(0);
+}
+// The same; dirty: without what is not finite in the tile.
+template <int D>
+__device__ __forceinline__ void multiply_finite(const TileRead<D>& r0, int off, const half8 (&f)[2], floatx16 (&acc)[D / 32], bool dirty) {
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+    for (int ks = 0; ks < 2; ++ks) {
+        half8 x[D / 32];
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.columns(off, i, ks), f[ks], acc[i], 0, 0, 0);
+        for (int i = 0; i < D / 32; ++i) x[i] = r0.columns(off, i, ks);
+        if (dirty) {
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) x[i] = finite_or_zero(x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i], f[ks], acc[i], 0, 0, 0);
     }
 }
 
@@ -108,15 +120,15 @@ __device__ __forceinline__ void clear(floatx16 (&x)[N]) {
 }
 
 // One block for a wave that owns keys: queries qb .. qb + 31 (rows 0 .. 31 of the pair q, do; stats: their lse log2(e) - 15 and, BLK
-// further on, delta) against the lane's key.  `hidden(query)` where cut.
-template <int D, typename Hidden>
-__device__ __forceinline__ void key_block(const TileRead<D>& r0, const float* stats, const half8 (&fk)[D / 16], const half8 (&fv)[D / 16], int qb, bool cut,
+// further on, delta) against the lane's key.  CUT: without the pairs that `hidden(query)`.
+template <int D, bool CUT, typename Hidden>
+__device__ __forceinline__ void key_block(const TileRead<D>& r0, const float* stats, const half8 (&fk)[D / 16], const half8 (&fv)[D / 16], int qb,
                                           Hidden hidden, floatx16 (&dk)[D / 32], floatx16 (&dv)[D / 32]) {
     constexpr float C2 = SCALE<D> * LOG2E;
     const int lh = (threadIdx.x & 63) >> 5;
     floatx16 S, P;
     products<D>(r0, fk, fv, S, P);
-    const bool dirty = cut && any_not_finite(S, P);
+    const bool dirty = CUT && any_not_finite(S, P);
 #pragma unroll
     for (int g4 = 0; g4 < 4; ++g4) {
         const float4 l4 = *reinterpret_cast<const float4*>(stats + 8 * g4 + 4 * lh), d4 = *reinterpret_cast<const float4*>(stats + BLK + 8 * g4 + 4 * lh);
@@ -125,17 +137,16 @@ __device__ __forceinline__ void key_block(const TileRead<D>& r0, const float* st
         for (int e = 0; e < 4; ++e) {
             S[4 * g4 + e] = __builtin_amdgcn_exp2f(fmaf(C2, S[4 * g4 + e], -lq[e]));
             P[4 * g4 + e] -= dq[e];
+            if constexpr (CUT) {
+                const bool h = hidden(qb + 8 * g4 + 4 * lh + e);
+                float p = S[4 * g4 + e], d = P[4 * g4 + e];
+                p = not_finite(d) ? NAN : p;
+                asm volatile("" : "+v"(p), "+v"(d));      // selects, no branches
+                S[4 * g4 + e] = h ? 0.f : p;
+                P[4 * g4 + e] = h ? 0.f : d;
+            }
         }
-    }
-    if (cut) {      // the branch stays one
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const bool h = hidden(qb + 8 * (e >> 2) + 4 * lh + (e & 3));
-            float p = h ? 0.f : (not_finite(P[e]) ? NAN : S[e]), d = h ? 0.f : P[e];
-            asm volatile("" : "+v"(p), "+v"(d));
-            S[e] = p;
-            P[e] = d;
-        }
+        if (g4 & 1) __builtin_amdgcn_sched_barrier(0);
     }
     uint32_t pp[8], pd[8];
 #pragma unroll
@@ -143,9 +154,15 @@ __device__ __forceinline__ void key_block(const TileRead<D>& r0, const float* st
         pp[e >> 1] = pack2(S[e], S[e + 1]);
         pd[e >> 1] = pack2(SCALE<D> / P_SCALE * S[e] * P[e], SCALE<D> / P_SCALE * S[e + 1] * P[e + 1]);
     }
+    __builtin_amdgcn_sched_barrier(0);
     const half8 fp[2] = {fragment_of(pp, 0), fragment_of(pp, 1)}, fd[2] = {fragment_of(pd, 0), fragment_of(pd, 1)};
-    multiply<D>(r0, TILE<D>, fp, dv, dirty);
-    multiply<D>(r0, 0, fd, dk, dirty);
+    if constexpr (CUT) {
+        multiply_finite<D>(r0, TILE<D>, fp, dv, dirty);
+        multiply_finite<D>(r0, 0, fd, dk, dirty);
+    } else {
+        multiply<D>(r0, TILE<D>, fp, dv);
+        multiply<D>(r0, 0, fd, dk);
+    }
 }
 
 template <int D>
@@ -242,43 +259,67 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
     floatx16 acc[D / 32];
     clear(acc);
 
-    auto half = [&](const TileRead<D>& r0, int k0, bool cut) {
+    // dS of keys k0 .. k0 + 31 as fragments
+    auto gradients = [&](const TileRead<D>& r0, int k0, auto cut, half8 (&f)[2], bool& dirty) {
         floatx16 S, P;
         products<D>(r0, fq, fd, S, P);
-        const bool dirty = cut && any_not_finite(S, P);
+        dirty = decltype(cut)::value && any_not_finite(S, P);
+        uint32_t pk[8];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             S[e] = SCALE<D> * __builtin_amdgcn_exp2f(fmaf(C2, S[e], -lq));
             P[e] -= delta;
-        }
-        if (cut) {      // the branch stays one
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
+            if constexpr (decltype(cut)::value) {
                 const int key = k0 + 8 * (e >> 2) + 4 * lh + (e & 3);
-                const bool h = key > query || (query - key >= window && key >= sinks);
-                float p = h ? 0.f : S[e], d = h ? 0.f : P[e];
-                asm volatile("" : "+v"(p), "+v"(d));
-                S[e] = p;
-                P[e] = d;
+                const bool h = key > query | (query - key >= window & key >= sinks);
+                float p = S[e], d = P[e];
+                asm volatile("" : "+v"(p), "+v"(d));      // selects, no branches
+                S[e] = h ? 0.f : p;
+                P[e] = h ? 0.f : d;
             }
         }
-        uint32_t pk[8];
 #pragma unroll
         for (int e = 0; e < 16; e += 2) pk[e >> 1] = pack2(S[e] * P[e], S[e + 1] * P[e + 1]);
-        const half8 f[2] = {fragment_of(pk, 0), fragment_of(pk, 1)};
-        multiply<D>(r0, 0, f, acc, dirty);
+        __builtin_amdgcn_sched_barrier(0);
+        f[0] = fragment_of(pk, 0);
+        f[1] = fragment_of(pk, 1);
     };
 
-    for (int it = 0; it < tiles; ++it) {
-        const int buf = it & 1, k0 = tile_at(it) * BLK;
+    int it = 0;
+    auto begin = [&]() {
         // the tiles have landed; everybody is done with the other pair
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (it + 1 < tiles) fetch(tile_at(it + 1), buf ^ 1);      // in flight while this pair is multiplied
-        if (!active) continue;
+        if (it + 1 < tiles) fetch(tile_at(it + 1), (it + 1) & 1);      // in flight while this pair is multiplied
+        return rd.at((it & 1) * PAIR<D>);
+    };
+    // the tiles that every query of the workgroup sees whole
+    const int whole0 = (max(0, q0 + ROWS - window) + BLK - 1) / BLK, whole1 = q0 / BLK - 1;
+    while (it < tiles) {
+        for (; it < tiles && !(it >= extra && tile_at(it) >= whole0 && tile_at(it) <= whole1); ++it) {
+            const int k0 = tile_at(it) * BLK;
+            const TileRead<D> r0 = begin();
+            if (!active) continue;
 #pragma nounroll
-        for (int h = 0; h < 2; ++h) {
-            const Seen x = seen(qw, k0 + 32 * h, window, sinks);
-            if (x != NONE) half(rd.at(buf * PAIR<D> + 32 * h * D), k0 + 32 * h, x == SOME);
+            for (int h = 0; h < 2; ++h) {
+                if (seen(qw, k0 + 32 * h, window, sinks) == NONE) continue;
+                const TileRead<D> r1 = r0.at(32 * h * D);
+                half8 f[2];
+                bool dirty;
+                gradients(r1, k0 + 32 * h, std::true_type{}, f, dirty);
+                multiply_finite<D>(r1, 0, f, acc, dirty);
+            }
+        }
+        for (; it < tiles && tile_at(it) <= whole1; ++it) {
+            const TileRead<D> r0 = begin();
+            if (!active) continue;
+#pragma nounroll
+            for (int h = 0; h < 2; ++h) {
+                const TileRead<D> r1 = r0.at(32 * h * D);
+                half8 f[2];
+                bool dirty;
+                gradients(r1, 0, std::false_type{}, f, dirty);
+                multiply<D>(r1, 0, f, acc);
+            }
         }
     }
     if (active) store_rows(acc, query < s.len ? a.dqkv + t * ld + (int64_t)n * D : nullptr);
@@ -325,25 +366,42 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
     clear(dk);
     clear(dv);
     const TileRead<D> rd(lds0);
-    auto hidden = [&](int query) { return query < key || query - key >= window; };
+    auto hidden = [&](int query) { return query < key | query - key >= window; };
 
-    int tile = first, n = kv * r;
-    for (int it = 0; it < steps; ++it) {
-        const int buf = it & 1, qb = tile * BLK;
+    int it = 0, tile = first, n = kv * r;      // the pair that is next
+    auto begin = [&](int& buf) {
+        buf = it & 1;
         tiles.keep_stats(buf);
         // the tiles have landed; everybody is done with the other pair
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        ++it;
         if (++tile > last) {
             tile = first;
             ++n;
         }
-        if (it + 1 < steps) tiles.fetch(tile, n, buf ^ 1);      // in flight while this pair is multiplied
-        if (!active) continue;
+        if (it < steps) tiles.fetch(tile, n, buf ^ 1);      // in flight while this pair is multiplied
+    };
+    // the query tiles that see every key of the workgroup
+    const int whole0 = k0 / BLK + 2, whole1 = (k0 + window - BLK) / BLK;
+    auto whole = [&]() { return tile >= whole0 && tile <= whole1; };
+    while (it < steps) {
+        while (it < steps && !whole()) {
+            const int qb = tile * BLK;
+            int buf;
+            begin(buf);
+            if (!active) continue;
 #pragma nounroll
-        for (int h = 0; h < 2; ++h) {
-            const Seen x = seen(qb + 32 * h, kw, window, 0);
-            if (x != NONE)
-                key_block<D>(rd.at(buf * PAIR<D> + 32 * h * D), stats + 2 * buf * BLK + 32 * h, fk, fv, qb + 32 * h, x == SOME, hidden, dk, dv);
+            for (int h = 0; h < 2; ++h)
+                if (seen(qb + 32 * h, kw, window, 0) != NONE)
+                    key_block<D, true>(rd.at(buf * PAIR<D> + 32 * h * D), stats + 2 * buf * BLK + 32 * h, fk, fv, qb + 32 * h, hidden, dk, dv);
+        }
+        while (it < steps && whole()) {
+            int buf;
+            begin(buf);
+            if (!active) continue;
+#pragma nounroll
+            for (int h = 0; h < 2; ++h)
+                key_block<D, false>(rd.at(buf * PAIR<D> + 32 * h * D), stats + 2 * buf * BLK + 32 * h, fk, fv, 0, hidden, dk, dv);
         }
     }
     if (!active) return;
@@ -420,7 +478,7 @@ __global__ __launch_bounds__(128, 1) void window_attention_far_kernel(win::BwdAr
         }
         if (it + 1 < steps) tiles.fetch(tile, n, buf ^ 1);
         if (qb + 31 - kw < window) continue;      // none of them
-        key_block<D>(rd.at(buf * PAIR<D>), stats + 2 * buf * BLK + 32 * wave, fk, fv, qb, qb - (kw + 31) < window, hidden, dk, dv);
+        key_block<D, true>(rd.at(buf * PAIR<D>), stats + 2 * buf * BLK + 32 * wave, fk, fv, qb, hidden, dk, dv);
     }
     // the two waves' sums
     float* xch = reinterpret_cast<float*>(smem) + lane;      // [dk | dv][D / 2][64 lanes]: as much as a pair of tiles

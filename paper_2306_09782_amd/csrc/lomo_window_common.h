@@ -86,7 +86,7 @@ __device__ __forceinline__ int swz(int r) {
 // descriptor ends behind the last one.  Rows are `ld` elements apart, 64 of them less than 4 GiB.
 template <int D>
 struct TileLoad {
-    static constexpr int RPI = 512 / D;              // rows that an instruction of a wave fetches
+    static constexpr int RPI = 512 / D;              // rows that an instruction of a wave fetches; a multiple of 16 to a wave
     uint32_t voff, ld2;
     __device__ __forceinline__ TileLoad(int64_t ld) {
         const int lane = threadIdx.x & 63, rr = lane / (D / 8), c = lane % (D / 8);
@@ -95,16 +95,18 @@ struct TileLoad {
     }
     template <int WAVES = 4>
     __device__ __forceinline__ void issue(const uint16_t* base, int rows, uint32_t tile, int wave) const {
-        const uint32_t n = (uint32_t)min(max(rows, 0), BLK);
-        const auto srd = dma::make_srd(base, n == 0 ? 0u : (n - 1) * ld2 + 2u * D);
         constexpr int PER = BLK / RPI / WAVES;
+        const int left = min(rows, BLK) - RPI * PER * wave;      // rows of the sequence among this wave's
+        base += (int64_t)(RPI * PER * wave) * (ld2 / 2);
         // instruction it fetches rows RPI (PER wave + it) ..; their swizzles differ from those of rows 0 .. in the low two chunk bits
 #pragma unroll
         for (int it = 0; it < PER; ++it) {
-            const int k = PER * wave + it, r0 = RPI * k;
-            uint32_t v = voff ^ (uint32_t)(((r0 >> 2) & 3) * 16);
-            asm volatile("" : "+v"(v));
-            dma::dma16(v + (uint32_t)r0 * ld2, srd, 0u, tile + (uint32_t)k * 1024u);
+            const int n = left - RPI * it;
+            const auto srd = dma::make_srd(base, n <= 0 ? 0u : (uint32_t)(min(n, RPI) - 1) * ld2 + 2u * D);
+            uint32_t v = voff ^ (uint32_t)(((RPI * it >> 2) & 3) * 16);
+            asm volatile("" : "+v"(v));      // formed again each time, not kept in registers
+            dma::dma16(v, srd, 0u, tile + (uint32_t)(PER * wave + it) * 1024u);
+            base += (int64_t)RPI * (ld2 / 2);
         }
     }
 };
@@ -186,6 +188,20 @@ __device__ __forceinline__ half8 finite_or_zero(half8 x) {
         w[e] &= ~(bad * 0xffffu);
     }
     return __builtin_bit_cast(half8, w);
+}
+// 1 for inf, 64 for -inf, 4096 for NaN, 0 for the rest; up to 32 of these added are told apart again.
+__device__ __forceinline__ half8 not_finite_code(half8 x) {
+    half8 c;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float f = (float)x[e];
+        c[e] = f == INFINITY ? (_Float16)1.f : f == -INFINITY ? (_Float16)64.f : f != f ? (_Float16)4096.f : (_Float16)0.f;
+    }
+    return c;
+}
+__device__ __forceinline__ float sum_of_codes(float sum) {
+    const uint32_t n = (uint32_t)sum, up = n & 63u, down = (n >> 6) & 63u;
+    return n >= 4096u || (up && down) ? NAN : up ? INFINITY : down ? -INFINITY : 0.f;
 }
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 

@@ -4,9 +4,7 @@
 //   o_i = sum_j exp(S_ij - lse_i) v_j
 //
 // One workgroup per (128 queries, head) walks the pairs of key and value tiles (64 keys) that the window of its queries reaches, the
-// tile of the sinks first where that is left of them; one pass with a running maximum and sum.  The keys of the even and of the odd halves of
-// the tiles have a maximum, a sum and an accumulator of their own (see lomo_attention_fwd.hip: less is rounded away), put together at
-// the end.  Workgroups are numbered so that the heads of a group and neighbouring queries run on one XCD at a time.  Probabilities are
+// tile of the sinks first where that is left of them; one pass with a running maximum and sum.  Workgroups are numbered so that the heads of a group and neighbouring queries run on one XCD at a time.  Probabilities are
 // rounded to fp16 relative to the running maximum, as the matrix cores take them; sums and accumulators are fp32; o is rounded once.
 // Deterministic, and independent of what else is in the batch.
 //
@@ -76,130 +74,148 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
     half8 fq[D / 16];
     if (active) load_fragments<D>(fq, gq + (int64_t)min(query, s.len - 1) * ld);
 
-    // by half of the tiles; log2 domain; l_run is this lane's share (its half of the keys)
+    // log2 domain; l_run is this lane's share (its half of the keys)
     constexpr int NC = D / 32;
-    floatx16 accO[2][NC];
-    float m_run[2], l_run[2];
+    floatx16 O[NC];
+    float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        m_run[h] = -INFINITY;
-        l_run[h] = 0.f;
+    for (int i = 0; i < NC; ++i)
 #pragma unroll
-        for (int i = 0; i < NC; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) accO[h][i][e] = 0.f;
-    }
+        for (int e = 0; e < 16; ++e) O[i][e] = 0.f;
 
-    auto scores = [&](const TileRead<D>& r0, floatx16& S) {
+    // Scores of keys 32 h .. + 31 of a pair: S[e] <-> key 8 (e / 4) + 4 lh + e % 4 of these.
+    auto scores = [&](const TileRead<D>& r0, int h, floatx16& S) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) S[e] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) S = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.rows(0, ks), fq[ks], S, 0, 0, 0);
+        for (int ks = 0; ks < D / 16; ++ks) S = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.rows(32 * h * D, ks), fq[ks], S, 0, 0, 0);
     };
-    // What keys k0 .. k0 + 31 (S[e] <-> key k0 + 8 (e / 4) + 4 lh + e % 4) add to sum and output.
-    auto half = [&](const TileRead<D>& r0, int k0, bool cut, floatx16& S, floatx16 (&O)[NC], float& m_run, float& l_run) {
-        auto hidden = [&](int key) { return key > query || (query - key >= window && key >= sinks); };
-        float scale = C2, bmax = -INFINITY;
-        if (cut) {      // scaled and masked; the branch stays one
-            scale = 1.f;
+    // From scores to probabilities relative to the running maximum, in fp16.  The maximum moves only where it has grown by more than
+    // SLACK: probabilities stay below 2^SLACK, and most tiles leave sum and output as they are.
+    constexpr float SLACK = 8.f;
+    auto probabilities = [&](floatx16 (&S)[2], uint32_t (&pk)[2][8]) {
+        float top = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                float x = hidden(k0 + 8 * (e >> 2) + 4 * lh + (e & 3)) ? -INFINITY : S[e] * C2;
-                asm volatile("" : "+v"(x));
-                S[e] = x;
-            }
-        }
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) bmax = fmaxf(bmax, S[e]);
-        {
-            const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(bmax), __float_as_uint(bmax), false, false);
-            bmax = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-        }
-        const float m_new = fmaxf(m_run, bmax * scale);
-        const float m_ref = (m_new == -INFINITY) ? 0.f : m_new;      // a query that has seen no key yet
-        float alpha = 1.f;
-        if (__any(m_new > m_run)) {
-            alpha = __builtin_amdgcn_exp2f(m_run - m_ref);
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, S[h][e]);
+        const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * C2;
+        if (__any(top > m_run + SLACK)) {
+            const float m_new = fmaxf(m_run, top), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
 #pragma unroll
             for (int i = 0; i < NC; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) O[i][e] *= alpha;
+            l_run *= alpha;
             m_run = m_new;
         }
-        float psum = 0.f;
-        uint32_t pk[8];
+        const float m_ref = m_run == -INFINITY ? 0.f : m_run;      // a query that has seen no key yet
+        float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(S[e], scale, -m_ref)), p1 = __builtin_amdgcn_exp2f(fmaf(S[e + 1], scale, -m_ref));
-            psum += p0 + p1;
-            pk[e >> 1] = pack2(p0, p1);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(S[h][e], C2, -m_ref)), p1 = __builtin_amdgcn_exp2f(fmaf(S[h][e + 1], C2, -m_ref));
+                sum += p0 + p1;
+                pk[h][e >> 1] = pack2(p0, p1);
+            }
+        l_run += sum;
+    };
+
+    int it = 0;
+    auto begin = [&]() {
+        // the tiles have landed; everybody is done with the other pair
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (it + 1 < tiles) fetch(tile_at(it + 1), (it + 1) & 1);      // in flight while this pair is multiplied
+        return rd.at((it & 1) * PAIR<D>);
+    };
+    // the tiles that every query of the workgroup sees whole
+    const int whole0 = (max(0, q0 + ROWS - window) + BLK - 1) / BLK, whole1 = q0 / BLK - 1;
+    while (it < tiles) {
+        for (; it < tiles && !(it >= extra && tile_at(it) >= whole0 && tile_at(it) <= whole1); ++it) {
+            const int k0 = tile_at(it) * BLK;
+            const TileRead<D> r0 = begin();
+            if (!active) continue;
+            const Seen seen_of[2] = {seen(qw, k0, window, sinks), seen(qw, k0 + 32, window, sinks)};
+            if (seen_of[0] == NONE && seen_of[1] == NONE) continue;
+            auto hidden = [&](int key) { return key > query | (query - key >= window & key >= sinks); };
+            floatx16 S[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (seen_of[h] != NONE) scores(r0, h, S[h]);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const bool no = seen_of[h] == NONE | hidden(k0 + 32 * h + 8 * (e >> 2) + 4 * lh + (e & 3));
+                    S[h][e] = no ? -INFINITY : S[h][e];
+                }
+            }
+            uint32_t pk[2][8];
+            probabilities(S, pk);
+#pragma nounroll
+            for (int h = 0; h < 2; ++h) {
+                if (seen_of[h] == NONE) continue;
+                const TileRead<D> r1 = r0.at(32 * h * D);
+                const bool dirty = any_not_finite<D>(r1, TILE<D>);
+                uint32_t own[8], see[8];
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const int key = k0 + 32 * h + 8 * (e >> 2) + 4 * lh + (e & 3);
+                    own[e >> 1] = h == 0 ? pk[0][e >> 1] : pk[1][e >> 1];
+                    see[e >> 1] = (hidden(key) ? 0u : 0x3c00u) | (hidden(key + 1) ? 0u : 0x3c000000u);
+                }
+                const half8 fp[2] = {fragment_of(own, 0), fragment_of(own, 1)};
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    half8 v[2] = {r1.columns(TILE<D>, i, 0), r1.columns(TILE<D>, i, 1)};
+                    floatx16 n;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) n[e] = 0.f;
+                    if (dirty) {      // what is not finite is left out, and added to the queries that see its key
+                        const half8 fs[2] = {fragment_of(see, 0), fragment_of(see, 1)};
+#pragma unroll
+                        for (int ks = 0; ks < 2; ++ks) {
+                            n = __builtin_amdgcn_mfma_f32_32x32x16_f16(not_finite_code(v[ks]), fs[ks], n, 0, 0, 0);
+                            v[ks] = finite_or_zero(v[ks]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) O[i][e] += sum_of_codes(n[e]);
+                    }
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks) O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[ks], fp[ks], O[i], 0, 0, 0);
+                }
+            }
         }
-        l_run = fmaf(l_run, alpha, psum);
-        const bool dirty = cut && any_not_finite<D>(r0, TILE<D>);
-        // o^T[column][query] += v^T[column][key] p^T[key][query], 16 keys at a time
+        for (; it < tiles && tile_at(it) <= whole1; ++it) {
+            const TileRead<D> r0 = begin();
+            if (!active) continue;
+            floatx16 S[2];
+            scores(r0, 0, S[0]);
+            scores(r0, 1, S[1]);
+            uint32_t pk[2][8];
+            probabilities(S, pk);
+            // o^T[column][query] += v^T[column][key] p^T[key][query], 16 keys at a time
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            const half8 fp = fragment_of(pk, ks);
-            if (dirty) {
-#pragma unroll
-                for (int i = 0; i < NC; ++i)
-                    O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(finite_or_zero(r0.columns(TILE<D>, i, ks)), fp, O[i], 0, 0, 0);
-            } else {
+            for (int ks = 0; ks < 4; ++ks) {
+                const half8 fp = fragment_of(pk[ks >> 1], ks & 1);
 #pragma unroll
                 for (int i = 0; i < NC; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.columns(TILE<D>, i, ks), fp, O[i], 0, 0, 0);
             }
         }
-        if (dirty) {      // what is not finite, to the queries that see its key
-            const uint32_t block = r0.row_rd - 2u * (uint32_t)(l32 * D + ((8 * lh) ^ (swz<D>(l32) << 3))) + 2u * TILE<D>;
-#pragma nounroll
-            for (int key = 0; key < 32; ++key) {
-#pragma unroll
-                for (int i = 0; i < NC; ++i)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int c = 32 * i + 8 * (e >> 2) + 4 * lh + (e & 3);
-                        const float x = (float)*(__attribute__((address_space(3))) const _Float16*)(block + 2u * (uint32_t)(key * D + (c ^ (swz<D>(key) << 3))));
-                        if (not_finite(x) && !hidden(k0 + key)) O[i][e] += x;
-                    }
-            }
-        }
-    };
-
-    for (int it = 0; it < tiles; ++it) {
-        const int buf = it & 1, k0 = tile_at(it) * BLK;
-        // the tiles have landed; everybody is done with the other pair
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (it + 1 < tiles) fetch(tile_at(it + 1), buf ^ 1);      // in flight while this pair is multiplied
-        if (!active) continue;
-        const Seen s0 = seen(qw, k0, window, sinks), s1 = seen(qw, k0 + 32, window, sinks);
-        const TileRead<D> r0 = rd.at(buf * PAIR<D>), r1 = rd.at(buf * PAIR<D> + 32 * D);
-        floatx16 S0, S1;
-        if (s0 != NONE) scores(r0, S0);
-        if (s1 != NONE) scores(r1, S1);
-        if (s0 != NONE) half(r0, k0, s0 == SOME, S0, accO[0], m_run[0], l_run[0]);
-        if (s1 != NONE) half(r1, k0 + 32, s1 == SOME, S1, accO[1], m_run[1], l_run[1]);
     }
 
-    // ---- the two halves' common maximum and total sum (every query sees itself), then o
+    // ---- the total sum (every query sees itself), then o
     if (!active) return;
-    float l[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run[h]), __float_as_uint(l_run[h]), false, false);
-        l[h] = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    }
-    const float mt = fmaxf(m_run[0], m_run[1]);
-    const float e0 = __builtin_amdgcn_exp2f(m_run[0] - mt), e1 = __builtin_amdgcn_exp2f(m_run[1] - mt);
-    const float lt = fmaf(l[0], e0, l[1] * e1);
-    const float f0 = e0 / lt, f1 = e1 / lt;
+    const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+    const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]), f = 1.f / l;
 #pragma unroll
     for (int i = 0; i < NC; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) accO[0][i][e] = fmaf(accO[0][i][e], f0, accO[1][i][e] * f1);
+        for (int e = 0; e < 16; ++e) O[i][e] *= f;
     const bool own = query < s.len;
     const int64_t t = (int64_t)s.start + query;
-    store_rows(accO[0], own ? a.o + (t * a.b.h + n) * D : nullptr);
-    if (own && lh == 0) a.lse[t * a.b.h + n] = (mt + __builtin_amdgcn_logf(lt)) * LN2;
+    store_rows(O, own ? a.o + (t * a.b.h + n) * D : nullptr);
+    if (own && lh == 0) a.lse[t * a.b.h + n] = (m_run + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 int64_t window_attention_pieces(int64_t T, int64_t B) { return win::pieces(T, B, win::ROWS, 1); }
