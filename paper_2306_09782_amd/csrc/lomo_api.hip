@@ -20,7 +20,7 @@ inline bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) 
 inline bool window_sizes_ok(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks) {
     if (T < 0 || B < 0 || h <= 0 || g <= 0 || h % g != 0 || (d != 64 && d != 128) || sinks < 0 || sinks > 64) return false;
     if (T > (1 << 30) || B > (1 << 24) || h > (1 << 16)) return false;      // with this, 64 rows stay below 4 GiB
-    return window_attention_pieces(T, B) * h <= 0x7fffffff;
+    return window_attention_grid(T, B, h, g, d, sinks) <= 0x7fffffff;
 }
 inline float step_size(float lr, float inv_loss_scale, float clip_coef) {
     return (float)((double)lr * (double)clip_coef * (double)inv_loss_scale);

@@ -27,7 +27,6 @@ namespace lomo {
 
 namespace attn {
 
-constexpr int XCH_BYTES = 4 * 2 * 64 * 16;                      // SPLIT = 2: two fragments of each wave
 constexpr int STAT_BYTES = 2 * 2 * BLK * 4;                     // lse and delta of a pair's queries
 template <int SPLIT>
 constexpr int DQ_LDS_BYTES = LDS_BYTES + (SPLIT == 2 ? XCH_BYTES : 0);
@@ -179,26 +178,6 @@ __device__ __forceinline__ void key_gradients(const TileRead& r0, const float* s
     }
     __builtin_amdgcn_sched_barrier(0);
 }
-
-// The exchange of SPLIT = 2: two fragments of this wave, of its partner (the wave with the same rows and the other half).
-struct Exchange {
-    half8 *own, *other;
-    __device__ __forceinline__ Exchange(uint16_t* lds, int wave) {
-        half8* x = reinterpret_cast<half8*>(lds) + (threadIdx.x & 63);
-        own = x + wave * 128;
-        other = x + (wave ^ 2) * 128;
-    }
-    __device__ __forceinline__ void put(const half8 (&f)[2]) const {
-        own[0] = f[0];
-        own[64] = f[1];
-    }
-    __device__ __forceinline__ void get(half8 (&f)[2]) const {
-        f[0] = other[0];
-        f[1] = other[64];
-    }
-};
-// LDS writes are visible to the other waves; the moving tiles' loads stay in flight
-__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 }  // namespace attn
 

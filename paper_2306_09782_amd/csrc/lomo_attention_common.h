@@ -194,6 +194,27 @@ __device__ __forceinline__ void store_rows(const floatx16 (&acc)[N], uint16_t* r
     }
 }
 
+// The exchange of waves that share rows: two fragments of this wave, of its partner (the wave with the same rows and the other half).
+constexpr int XCH_BYTES = 4 * 2 * 64 * 16;
+struct Exchange {
+    half8 *own, *other;
+    __device__ __forceinline__ Exchange(uint16_t* lds, int wave) {
+        half8* x = reinterpret_cast<half8*>(lds) + (threadIdx.x & 63);
+        own = x + wave * 128;
+        other = x + (wave ^ 2) * 128;
+    }
+    __device__ __forceinline__ void put(const half8 (&f)[2]) const {
+        own[0] = f[0];
+        own[64] = f[1];
+    }
+    __device__ __forceinline__ void get(half8 (&f)[2]) const {
+        f[0] = other[0];
+        f[1] = other[64];
+    }
+};
+// LDS writes are visible to the other waves; the moving tiles' loads stay in flight
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // Waves of a call that is not split, per CU.  Below four, one for every SIMD, the chip has room for twice as many; with more a call of
 // long walks still ends sooner when they are halved.
 inline double waves_per_cu(int64_t B, int64_t s, int64_t nh) { return (double)(s / 32 * nh * B) / (double)cu_count(); }

@@ -4,11 +4,11 @@
 //   P_ij = exp(q_i . k_j / sqrt(d) - lse_i),   dP_ij = do_i . v_j,   delta_i = do_i . o_i,   dS = P (dP - delta) / sqrt(d)
 //   dq_i = sum_j dS_ij k_j;   dk_j = sum over the queries i of all heads of the group dS_ij q_i;   dv_j likewise of P_ij do_i
 //
-// Four deterministic kernels, no atomics.  The first: a workgroup per (128 queries, head) forms delta, walks the tiles of keys
-// that the window reaches, and the sinks', and accumulates dq.  The second: a workgroup per (128 keys, key head) walks the query tiles
+// Three deterministic kernels, no atomics.  The first: a workgroup per (128 queries, head) forms delta, walks the tiles of keys
+// that the window reaches, and the sinks', and accumulates dq.  The second: a workgroup per (64 keys, key head) walks the query tiles
 // whose window reaches the keys, for each head of the group, and accumulates dk and dv.  The sinks have queries beyond their window, up to
-// the whole sequence: the third kernel sums over those, FAR_ROWS queries of all heads of a group to a workgroup, each result a
-// slot of `sinks` fp32 rows in the workspace, where the second puts its own sums of these rows; the fourth adds the slots in order
+// the whole sequence: further workgroups of the second kernel sum over those, FAR_ROWS queries of all heads of a group each, into a
+// slot of `sinks` fp32 rows in the workspace, where the sums over the window go too for these rows; the third adds the slots in order
 // and rounds.  All recompute S, P, dP, dS in blocks of 32 x 32 per wave with the wave's own rows along the lanes.
 //
 // fp32 accumulation on the matrix cores.  P and dS pass through fp16 before the products that consume them; P is held times 2^15 there,
@@ -16,6 +16,7 @@
 // cuts look for inf and NaN and take them out of the products, so that a pair which the mask hides adds nothing.
 #include "lomo_window_common.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace lomo {
@@ -34,10 +35,12 @@ struct BwdArgs {
     float* delta;             // [T x h], written by the dq kernel
     float* slots;             // [slot][g][dk | dv][sinks][D]
     uint16_t* dqkv;           // [T x (h + 2 g) D]
-    int numbers, total_q, total_k;      // of 128-row pieces; of workgroups
-    int slot_numbers;
+    int numbers_q, numbers_k, total_q, total_k;      // pieces of 128 queries, of 64 keys; workgroups for them
+    int far;                                         // workgroups for the queries beyond the sinks' window
 };
 
+// Workgroups of the third kernel for a sequence and key head.
+__host__ __device__ __forceinline__ constexpr int sinks_blocks(int sinks, int d) { return (2 * sinks * d + 255) / 256; }
 // The sequence has pairs of a sink and a query beyond its window.
 __device__ __forceinline__ bool has_far(const Batch& b, int len) { return b.sinks > 0 && len > b.window; }
 template <int D>
@@ -119,34 +122,33 @@ __device__ __forceinline__ void clear(floatx16 (&x)[N]) {
         for (int e = 0; e < 16; ++e) x[i][e] = 0.f;
 }
 
-// One block for a wave that owns keys: queries qb .. qb + 31 (rows 0 .. 31 of the pair q, do; stats: their lse log2(e) - 15 and, BLK
-// further on, delta) against the lane's key.  CUT: without the pairs that `hidden(query)`.
-template <int D, bool CUT, typename Hidden>
-__device__ __forceinline__ void key_block(const TileRead<D>& r0, const float* stats, const half8 (&fk)[D / 16], const half8 (&fv)[D / 16], int qb,
-                                          Hidden hidden, floatx16 (&dk)[D / 32], floatx16 (&dv)[D / 32]) {
+// P (times P_SCALE) and dS of a block as fragments, for a wave that owns keys: queries qb .. qb + 31 (rows 0 .. 31 of the pair q, do;
+// stats: their lse log2(e) - 15 and, BLK further on, delta) against the lane's key.  CUT: without the pairs whose distance is not one of the
+// `reach` from `near` on.
+template <int D, bool CUT>
+__device__ __forceinline__ void key_gradients(const TileRead<D>& r0, const float* stats, const half8 (&fk)[D / 16], const half8 (&fv)[D / 16],
+                                              int distance, uint32_t reach, half8 (&fp)[2], half8 (&fd)[2]) {
     constexpr float C2 = SCALE<D> * LOG2E;
     const int lh = (threadIdx.x & 63) >> 5;
     floatx16 S, P;
     products<D>(r0, fk, fv, S, P);
-    const bool dirty = CUT && any_not_finite(S, P);
 #pragma unroll
     for (int g4 = 0; g4 < 4; ++g4) {
         const float4 l4 = *reinterpret_cast<const float4*>(stats + 8 * g4 + 4 * lh), d4 = *reinterpret_cast<const float4*>(stats + BLK + 8 * g4 + 4 * lh);
         const float lq[4] = {l4.x, l4.y, l4.z, l4.w}, dq[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            S[4 * g4 + e] = __builtin_amdgcn_exp2f(fmaf(C2, S[4 * g4 + e], -lq[e]));
-            P[4 * g4 + e] -= dq[e];
+            float p = __builtin_amdgcn_exp2f(fmaf(C2, S[4 * g4 + e], -lq[e])), d = P[4 * g4 + e] - dq[e];
             if constexpr (CUT) {
-                const bool h = hidden(qb + 8 * g4 + 4 * lh + e);
-                float p = S[4 * g4 + e], d = P[4 * g4 + e];
                 p = not_finite(d) ? NAN : p;
                 asm volatile("" : "+v"(p), "+v"(d));      // selects, no branches
-                S[4 * g4 + e] = h ? 0.f : p;
-                P[4 * g4 + e] = h ? 0.f : d;
+                const bool hidden = (uint32_t)(distance + 8 * g4 + e) >= reach;
+                p = hidden ? 0.f : p;
+                d = hidden ? 0.f : d;
             }
+            S[4 * g4 + e] = p;
+            P[4 * g4 + e] = d;
         }
-        if (g4 & 1) __builtin_amdgcn_sched_barrier(0);
     }
     uint32_t pp[8], pd[8];
 #pragma unroll
@@ -155,13 +157,10 @@ __device__ __forceinline__ void key_block(const TileRead<D>& r0, const float* st
         pd[e >> 1] = pack2(SCALE<D> / P_SCALE * S[e] * P[e], SCALE<D> / P_SCALE * S[e + 1] * P[e + 1]);
     }
     __builtin_amdgcn_sched_barrier(0);
-    const half8 fp[2] = {fragment_of(pp, 0), fragment_of(pp, 1)}, fd[2] = {fragment_of(pd, 0), fragment_of(pd, 1)};
-    if constexpr (CUT) {
-        multiply_finite<D>(r0, TILE<D>, fp, dv, dirty);
-        multiply_finite<D>(r0, 0, fd, dk, dirty);
-    } else {
-        multiply<D>(r0, TILE<D>, fp, dv);
-        multiply<D>(r0, 0, fd, dk);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+        fp[ks] = fragment_of(pp, ks);
+        fd[ks] = fragment_of(pd, ks);
     }
 }
 
@@ -169,7 +168,7 @@ template <int D>
 constexpr int DQ_LDS_BYTES = 2 * PAIR<D> * 2;
 constexpr int STAT_BYTES = 2 * 2 * BLK * 4;      // lse and delta of the queries of two pairs
 template <int D>
-constexpr int KEY_LDS_BYTES = DQ_LDS_BYTES<D> + STAT_BYTES;
+constexpr int KEY_LDS_BYTES = DQ_LDS_BYTES<D> + STAT_BYTES + attn::XCH_BYTES;
 
 // The moving pairs of the kernels that own keys: q and do of 64 queries of a head, and their lse and delta.  Rows behind the sequence are zeros with
 // an lse of infinity: their probabilities are 0.
@@ -214,8 +213,8 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
     const int window = a.b.window, sinks = a.b.sinks;
 
     // order: key heads, pieces, the heads of the group
-    const int place = place_of_block(a.total_q), r = a.b.h / a.b.g;
-    const int kv = place / (a.numbers * r), rest = place - kv * a.numbers * r;
+    const int place = place_of_block(a.total_q, blockIdx.x), r = a.b.h / a.b.g;
+    const int kv = place / (a.numbers_q * r), rest = place - kv * a.numbers_q * r;
     const int number = rest / r, n = kv * r + (rest - number * r);
     const int seq = sequence_of(a.b, number, ROWS, 1);
     if (seq < 0) return;
@@ -325,34 +324,65 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
     if (active) store_rows(acc, query < s.len ? a.dqkv + t * ld + (int64_t)n * D : nullptr);
 }
 
+// A workgroup has 64 keys and the queries whose distance to a key is within some bounds: of the first a.far workgroups the sinks and FAR_ROWS
+// queries beyond the window, of the others a block of keys and the queries whose window reaches it.  Two waves have the same 32 keys; each forms
+// P and dS of one half of the tile's queries, hands one of the two to the other through LDS, and sums dv (the first) or dk over all of them:
+// twice the workgroups of one that has both sums, of which a group of heads leaves few, and half the accumulators.
 template <int D>
 __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdArgs a) {
     using namespace win;
-    extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // lse and delta of two pairs of tiles; the pairs: Q, dO
+    extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // lse and delta of two pairs of tiles; the pairs: Q, dO; what waves exchange
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int l32 = lane & 31;
+    const int part = wave >> 1, l32 = lane & 31, lh = lane >> 5;
     float* stats = reinterpret_cast<float*>(smem);      // [pair][lse log2(e) - 15 | delta][64]
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(smem + STAT_BYTES / 2);
-    const int window = a.b.window;
+    uint16_t* tiles_at = smem + STAT_BYTES / 2;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)tiles_at;
+    const attn::Exchange xch(tiles_at + 2 * PAIR<D>, wave);
 
-    // order: key heads, pieces
-    const int place = place_of_block(a.total_k), r = a.b.h / a.b.g;
-    const int kv = place / a.numbers, number = place - kv * a.numbers;
-    const int seq = sequence_of(a.b, number, ROWS, 1);
-    if (seq < 0) return;
-    const Rows s = rows_of(a.b, seq);
-    const int nb = (s.len + ROWS - 1) / ROWS, at = number - first_piece(a.b, seq, ROWS, 1);
-    if (at >= nb) return;
-    const int k0 = at * ROWS, kw = k0 + 32 * wave;      // the longest walks first
-    const bool active = kw < s.len;
-    const int key = kw + l32;
+    const int r = a.b.h / a.b.g;
+    int seq, kv, k0, near, first, last;      // keys from k0 on; query tiles; the distance of the nearest query
+    uint32_t reach;
+    float* slot = nullptr;
+    Rows s;
+    if ((int)blockIdx.x < a.far) {
+        const int number = blockIdx.x / a.b.g;
+        kv = blockIdx.x - number * a.b.g;
+        seq = sequence_of(a.b, number, FAR_ROWS, 2);
+        if (seq < 0) return;
+        s = rows_of(a.b, seq);
+        const int piece = number - first_piece(a.b, seq, FAR_ROWS, 2) - 1;      // the first number is for the sums of the block of keys
+        if (piece < 0 || !has_far(a.b, s.len)) return;
+        const int from = max((int64_t)piece * FAR_ROWS, (int64_t)a.b.window), to = min((int64_t)s.len, (int64_t)(piece + 1) * FAR_ROWS);
+        if (from >= to) return;
+        k0 = 0;
+        near = a.b.window;
+        reach = 0x7fffffffu;
+        first = from / BLK;
+        last = (to - 1) / BLK;
+        slot = slot_at<D>(a, number, kv);
+    } else {
+        // order: key heads, blocks
+        const int place = place_of_block(a.total_k, (int)blockIdx.x - a.far);
+        kv = place / a.numbers_k;
+        const int number = place - kv * a.numbers_k;
+        seq = sequence_of(a.b, number, BLK, 1);
+        if (seq < 0) return;
+        s = rows_of(a.b, seq);
+        k0 = (number - first_piece(a.b, seq, BLK, 1)) * BLK;      // the longest walks first
+        if (k0 >= s.len) return;
+        near = 0;
+        reach = (uint32_t)a.b.window;
+        first = k0 / BLK;
+        last = (int)min((int64_t)s.len - 1, (int64_t)k0 + BLK - 2 + a.b.window) / BLK;
+        if (k0 == 0 && has_far(a.b, s.len)) slot = slot_at<D>(a, first_piece(a.b, seq, FAR_ROWS, 2), kv);
+    }
+    const int kw = k0 + 32 * (wave & 1), key = kw + l32;
+    const bool active = kw < s.len && (near == 0 || kw < a.b.sinks);
     const int64_t ld = (int64_t)(a.b.h + 2 * a.b.g) * D;
     const int64_t t = (int64_t)s.start + min(key, s.len - 1);
 
-    // query tiles of one head, all heads of the group in turn
-    const int first = k0 / BLK, last = (int)min((int64_t)s.len - 1, (int64_t)k0 + ROWS - 2 + window) / BLK;
     const int per = last - first + 1, steps = per * r;
     QueryTiles<D, 4> tiles(a, s, lds0, stats);
     tiles.fetch(first, kv * r, 0);
@@ -362,15 +392,13 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
         load_fragments<D>(fk, a.qkv + t * ld + (int64_t)(a.b.h + kv) * D);
         load_fragments<D>(fv, a.qkv + t * ld + (int64_t)(a.b.h + a.b.g + kv) * D);
     }
-    floatx16 dk[D / 32], dv[D / 32];
-    clear(dk);
-    clear(dv);
+    floatx16 acc[D / 32];      // dv or dk
+    clear(acc);
     const TileRead<D> rd(lds0);
-    auto hidden = [&](int query) { return query < key | query - key >= window; };
 
     int it = 0, tile = first, n = kv * r;      // the pair that is next
-    auto begin = [&](int& buf) {
-        buf = it & 1;
+    auto begin = [&]() {
+        const int buf = it & 1;
         tiles.keep_stats(buf);
         // the tiles have landed; everybody is done with the other pair
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -380,153 +408,104 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
             ++n;
         }
         if (it < steps) tiles.fetch(tile, n, buf ^ 1);      // in flight while this pair is multiplied
+        return buf;
     };
-    // the query tiles that see every key of the workgroup
-    const int whole0 = k0 / BLK + 2, whole1 = (k0 + window - BLK) / BLK;
+    auto own_gradients = [&](int buf, int distance, auto cut, half8 (&f)[2]) {
+        half8 fp[2], fd[2];
+        key_gradients<D, decltype(cut)::value>(rd.at(buf * PAIR<D> + 32 * part * D), stats + 2 * buf * BLK + 32 * part, fk, fv, distance, reach, fp, fd);
+        if (part == 0) xch.put(fd);
+        else xch.put(fp);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) f[ks] = part == 0 ? fp[ks] : fd[ks];
+    };
+    // the query tiles that are within the bounds for every key of the workgroup
+    const int whole0 = (k0 + BLK - 1 + near + BLK - 1) / BLK, whole1 = near > 0 ? last : (k0 + a.b.window - BLK) / BLK;
     auto whole = [&]() { return tile >= whole0 && tile <= whole1; };
     while (it < steps) {
         while (it < steps && !whole()) {
-            const int qb = tile * BLK;
-            int buf;
-            begin(buf);
-            if (!active) continue;
+            const int qb = tile * BLK, buf = begin();
+            // distances in each half: between qb + 32 h - (kw + 31) and qb + 32 h + 31 - kw
+            auto some = [&](int h) { return active && qb + 32 * h + 31 - kw >= near && (near > 0 || qb + 32 * h - (kw + 31) < (int)reach); };
+            half8 f[2], g[2];
+            if (some(part)) own_gradients(buf, qb + 32 * part + 4 * lh - key - near, std::true_type{}, f);
+            attn::meet();
 #pragma nounroll
-            for (int h = 0; h < 2; ++h)
-                if (seen(qb + 32 * h, kw, window, 0) != NONE)
-                    key_block<D, true>(rd.at(buf * PAIR<D> + 32 * h * D), stats + 2 * buf * BLK + 32 * h, fk, fv, qb + 32 * h, hidden, dk, dv);
+            for (int h = 0; h < 2; ++h) {
+                if (!some(h)) continue;
+                const TileRead<D> r0 = rd.at(buf * PAIR<D> + (part == 0 ? TILE<D> : 0) + 32 * h * D);
+                xch.get(g);
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) g[ks] = h == part ? f[ks] : g[ks];
+                multiply_finite<D>(r0, 0, g, acc, any_not_finite<D>(r0, 0));
+            }
         }
         while (it < steps && whole()) {
-            int buf;
-            begin(buf);
+            const int buf = begin();
+            half8 f[2], g[2];
+            if (active) own_gradients(buf, 0, std::false_type{}, f);
+            attn::meet();
             if (!active) continue;
-#pragma nounroll
-            for (int h = 0; h < 2; ++h)
-                key_block<D, false>(rd.at(buf * PAIR<D> + 32 * h * D), stats + 2 * buf * BLK + 32 * h, fk, fv, 0, hidden, dk, dv);
+            const TileRead<D> r0 = rd.at(buf * PAIR<D> + (part == 0 ? TILE<D> : 0));
+            xch.get(g);
+            if (part == 0) {
+                multiply<D>(r0, 0, f, acc);
+                multiply<D>(r0, 32 * D, g, acc);
+            } else {
+                multiply<D>(r0, 0, g, acc);
+                multiply<D>(r0, 32 * D, f, acc);
+            }
         }
     }
     if (!active) return;
+    if (part == 0) {
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
+        for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) dv[i][e] *= 1.f / P_SCALE;
-    const bool own = key < s.len, sink = own && key < a.b.sinks && has_far(a.b, s.len);
-    uint16_t* out = own && !sink ? a.dqkv + t * ld + (int64_t)(a.b.h + kv) * D : nullptr;
-    store_rows(dk, out);
-    store_rows(dv, out == nullptr ? nullptr : out + (int64_t)a.b.g * D);
+            for (int e = 0; e < 16; ++e) acc[i][e] *= 1.f / P_SCALE;
+    }
+    const bool own = key < s.len, sink = own && key < a.b.sinks && slot != nullptr;
+    if (near == 0) store_rows(acc, own && !sink ? a.dqkv + t * ld + (int64_t)(a.b.h + (1 - part) * a.b.g + kv) * D : nullptr);
     if (sink) {
-        float* slot = slot_at<D>(a, first_piece(a.b, seq, FAR_ROWS, 2), kv) + (int64_t)key * D + 4 * ((threadIdx.x & 63) >> 5);
-        float* second = slot + (int64_t)a.b.sinks * D;
+        float* out = slot + (int64_t)((1 - part) * a.b.sinks + key) * D + 4 * lh;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-            for (int g4 = 0; g4 < 4; ++g4) {
-                *reinterpret_cast<float4*>(slot + 32 * i + 8 * g4) = {dk[i][4 * g4], dk[i][4 * g4 + 1], dk[i][4 * g4 + 2], dk[i][4 * g4 + 3]};
-                *reinterpret_cast<float4*>(second + 32 * i + 8 * g4) = {dv[i][4 * g4], dv[i][4 * g4 + 1], dv[i][4 * g4 + 2], dv[i][4 * g4 + 3]};
-            }
+            for (int g4 = 0; g4 < 4; ++g4)
+                *reinterpret_cast<float4*>(out + 32 * i + 8 * g4) = {acc[i][4 * g4], acc[i][4 * g4 + 1], acc[i][4 * g4 + 2], acc[i][4 * g4 + 3]};
     }
 }
 
-// The sinks and FAR_ROWS queries, those beyond the window; a wave has 32 of each tile's 64, a workgroup 32 sinks.
-template <int D>
-__global__ __launch_bounds__(128, 1) void window_attention_far_kernel(win::BwdArgs a) {
-    using namespace win;
-    extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // as above
-
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int l32 = lane & 31, lh = lane >> 5;
-    float* stats = reinterpret_cast<float*>(smem);
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(smem + STAT_BYTES / 2);
-    const int window = a.b.window, r = a.b.h / a.b.g;
-
-    const int parts = (a.b.sinks + 31) / 32;
-    const int number = blockIdx.x / (a.b.g * parts), rest = blockIdx.x - number * a.b.g * parts;
-    const int kv = rest / parts, kw = 32 * (rest - kv * parts);      // these sinks
-    const int seq = sequence_of(a.b, number, FAR_ROWS, 2);
-    if (seq < 0) return;
-    const Rows s = rows_of(a.b, seq);
-    const int piece = number - first_piece(a.b, seq, FAR_ROWS, 2) - 1;      // the first number is the second kernel's slot
-    if (piece < 0 || !has_far(a.b, s.len)) return;
-    const int from = max((int64_t)piece * FAR_ROWS, (int64_t)window), to = min((int64_t)s.len, (int64_t)(piece + 1) * FAR_ROWS);
-    if (from >= to || kw >= s.len) return;
-    const int64_t ld = (int64_t)(a.b.h + 2 * a.b.g) * D;
-    const int key = kw + l32;
-    const int64_t t = (int64_t)s.start + min(key, s.len - 1);
-
-    const int first = from / BLK, last = (to - 1) / BLK;
-    const int per = last - first + 1, steps = per * r;
-    QueryTiles<D, 2> tiles(a, s, lds0, stats);
-    tiles.fetch(first, kv * r, 0);
-
-    half8 fk[D / 16], fv[D / 16];
-    load_fragments<D>(fk, a.qkv + t * ld + (int64_t)(a.b.h + kv) * D);
-    load_fragments<D>(fv, a.qkv + t * ld + (int64_t)(a.b.h + a.b.g + kv) * D);
-    floatx16 dk[D / 32], dv[D / 32];
-    clear(dk);
-    clear(dv);
-    const TileRead<D> rd = TileRead<D>(lds0).at(32 * wave * D);
-    auto hidden = [&](int query) { return query - key < window; };
-
-    int tile = first, n = kv * r;
-    for (int it = 0; it < steps; ++it) {
-        const int buf = it & 1, qb = tile * BLK + 32 * wave;
-        tiles.keep_stats(buf);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (++tile > last) {
-            tile = first;
-            ++n;
-        }
-        if (it + 1 < steps) tiles.fetch(tile, n, buf ^ 1);
-        if (qb + 31 - kw < window) continue;      // none of them
-        key_block<D, true>(rd.at(buf * PAIR<D>), stats + 2 * buf * BLK + 32 * wave, fk, fv, qb, hidden, dk, dv);
-    }
-    // the two waves' sums
-    float* xch = reinterpret_cast<float*>(smem) + lane;      // [dk | dv][D / 2][64 lanes]: as much as a pair of tiles
-    __syncthreads();
-    if (wave == 1) {
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                xch[(16 * i + e) * 64] = dk[i][e];
-                xch[(D / 2 + 16 * i + e) * 64] = dv[i][e];
-            }
-    }
-    __syncthreads();
-    if (wave == 1 || key >= min(a.b.sinks, s.len)) return;
-    float* slot = slot_at<D>(a, number, kv) + (int64_t)key * D + 4 * lh;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int c = 32 * i + 8 * (e >> 2) + (e & 3);
-            slot[c] = dk[i][e] + xch[(16 * i + e) * 64];
-            slot[(int64_t)a.b.sinks * D + c] = (dv[i][e] + xch[(D / 2 + 16 * i + e) * 64]) * (1.f / P_SCALE);
-        }
-}
-
-// The sinks' dk and dv: the second kernel's sums and the third's, in order.
+// The sinks' dk and dv: the sums over their window and over the pieces beyond it, in order.  One thread per element.
 template <int D>
 __global__ __launch_bounds__(256) void window_attention_sinks_kernel(win::BwdArgs a) {
     using namespace win;
-    const int seq = blockIdx.x / a.b.g, kv = blockIdx.x - seq * a.b.g;
+    const int per = sinks_blocks(a.b.sinks, D), pair = blockIdx.x / per;
+    const int seq = pair / a.b.g, kv = pair - seq * a.b.g;
     const Rows s = rows_of(a.b, seq);
-    if (!has_far(a.b, s.len)) return;
+    const int i = (blockIdx.x - pair * per) * 256 + threadIdx.x;
+    const int which = i / (a.b.sinks * D), row = (i - which * a.b.sinks * D) / D, c = i % D;
+    if (!has_far(a.b, s.len) || which > 1 || row >= s.len) return;
     const int base = first_piece(a.b, seq, FAR_ROWS, 2);
     const int from = a.b.window / FAR_ROWS, to = (s.len - 1) / FAR_ROWS;
-    const int64_t ld = (int64_t)(a.b.h + 2 * a.b.g) * D;
     const int64_t step = (int64_t)a.b.g * 2 * a.b.sinks * D;
-    const int rows = min(a.b.sinks, s.len);
-    for (int i = threadIdx.x; i < 2 * rows * D; i += 256) {
-        const int which = i / (rows * D), row = (i - which * rows * D) / D, c = i % D;
-        const float* p = slot_at<D>(a, base, kv) + ((int64_t)which * a.b.sinks + row) * D + c;
-        float sum = *p;
-        for (int k = from; k <= to; ++k) sum += p[(k + 1) * step];
-        const _Float16 x = (_Float16)sum;
-        a.dqkv[((int64_t)s.start + row) * ld + (int64_t)(a.b.h + which * a.b.g + kv) * D + c] = __builtin_bit_cast(uint16_t, x);
+    const float* p = slot_at<D>(a, base, kv) + ((int64_t)which * a.b.sinks + row) * D + c;
+    float sum = *p;
+    for (int k = from; k <= to; k += 8) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = k + e <= to ? p[(k + e + 1) * step] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += x[e];
     }
+    const _Float16 x = (_Float16)sum;
+    a.dqkv[((int64_t)s.start + row) * (a.b.h + 2 * a.b.g) * D + (int64_t)(a.b.h + which * a.b.g + kv) * D + c] = __builtin_bit_cast(uint16_t, x);
 }
 
+int64_t window_attention_grid(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks) {
+    using namespace win;
+    const int64_t rows = pieces(T, B, ROWS, 1) * h, keys = (pieces(T, B, BLK, 1) + pieces(T, B, FAR_ROWS, 2)) * g;
+    return std::max(std::max(rows, keys), B * g * sinks_blocks((int)sinks, (int)d));
+}
 size_t window_attention_delta_bytes(int64_t T, int64_t h) { return ((size_t)T * h * 4 + 255) & ~(size_t)255; }
 size_t window_attention_ws_bytes(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks) {
     return window_attention_delta_bytes(T, h) + (size_t)(win::pieces(T, B, win::FAR_ROWS, 2) * g * 2 * sinks * d) * 4;
@@ -537,19 +516,14 @@ static hipError_t launch_backward_of(const win::BwdArgs& a, hipStream_t st) {
     using namespace win;
     auto dq = window_attention_dq_kernel<D>;
     auto dkdv = window_attention_dkdv_kernel<D>;
-    auto far = window_attention_far_kernel<D>;
     static const hipError_t cfg0 = allow_dynamic_lds(dq, DQ_LDS_BYTES<D>);
     if (cfg0 != hipSuccess) return cfg0;
     static const hipError_t cfg1 = allow_dynamic_lds(dkdv, KEY_LDS_BYTES<D>);
     if (cfg1 != hipSuccess) return cfg1;
-    static const hipError_t cfg2 = allow_dynamic_lds(far, KEY_LDS_BYTES<D>);
-    if (cfg2 != hipSuccess) return cfg2;
     hipLaunchKernelGGL(dq, dim3((unsigned)a.total_q), dim3(256), DQ_LDS_BYTES<D>, st, a);
-    hipLaunchKernelGGL(dkdv, dim3((unsigned)a.total_k), dim3(256), KEY_LDS_BYTES<D>, st, a);
-    if (a.b.sinks > 0 && a.b.T > a.b.window) {      // no sequence is longer than T
-        hipLaunchKernelGGL(far, dim3((unsigned)(a.slot_numbers * a.b.g * ((a.b.sinks + 31) / 32))), dim3(128), KEY_LDS_BYTES<D>, st, a);
-        hipLaunchKernelGGL(window_attention_sinks_kernel<D>, dim3((unsigned)(a.b.B * a.b.g)), dim3(256), 0, st, a);
-    }
+    hipLaunchKernelGGL(dkdv, dim3((unsigned)(a.far + a.total_k)), dim3(256), KEY_LDS_BYTES<D>, st, a);
+    if (a.far > 0)
+        hipLaunchKernelGGL(window_attention_sinks_kernel<D>, dim3((unsigned)(a.b.B * a.b.g * sinks_blocks(a.b.sinks, D))), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
@@ -561,10 +535,11 @@ hipError_t launch_window_attention_backward(const uint16_t* qkv, const uint16_t*
     a.qkv = qkv; a.o = o; a.dO = dO; a.lse = lse; a.dqkv = dqkv;
     a.delta = static_cast<float*>(ws);
     a.slots = reinterpret_cast<float*>(static_cast<char*>(ws) + window_attention_delta_bytes(T, h));
-    a.numbers = (int)win::pieces(T, B, win::ROWS, 1);
-    a.total_q = (int)(a.numbers * h);
-    a.total_k = (int)(a.numbers * g);
-    a.slot_numbers = (int)win::pieces(T, B, win::FAR_ROWS, 2);
+    a.numbers_q = (int)win::pieces(T, B, win::ROWS, 1);
+    a.numbers_k = (int)win::pieces(T, B, win::BLK, 1);
+    a.total_q = (int)(a.numbers_q * h);
+    a.total_k = (int)(a.numbers_k * g);
+    a.far = sinks > 0 && T > window ? (int)(win::pieces(T, B, win::FAR_ROWS, 2) * g) : 0;      // no sequence is longer than T
     return d == 128 ? launch_backward_of<128>(a, st) : launch_backward_of<64>(a, st);
 }
 

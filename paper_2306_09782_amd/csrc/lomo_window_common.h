@@ -65,10 +65,10 @@ __device__ __forceinline__ int sequence_of(const Batch& a, int i, int unit, int 
 }
 inline int64_t pieces(int64_t T, int64_t B, int64_t unit, int64_t more) { return T / unit + more * B; }
 
-// Place of this workgroup in an order of `total`, cut into one contiguous run for each XCD (blockIdx % 8), so that neighbours
+// Place of workgroup `block` in an order of `total`, cut into one contiguous run for each XCD (block % 8), so that neighbours
 // in the order meet in one L2.
-__device__ __forceinline__ int place_of_block(int total) {
-    const int x = (int)(blockIdx.x & 7), local = (int)(blockIdx.x >> 3);
+__device__ __forceinline__ int place_of_block(int total, int block) {
+    const int x = block & 7, local = block >> 3;
     const int q = total >> 3, r = total & 7;
     return x * q + (x < r ? x : r) + local;
 }

@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
     const int window = a.b.window, sinks = a.b.sinks;
 
     // order: key heads, pieces, the heads of the group
-    const int place = place_of_block(a.total), r = a.b.h / a.b.g;
+    const int place = place_of_block(a.total, blockIdx.x), r = a.b.h / a.b.g;
     const int kv = place / (a.numbers * r), rest = place - kv * a.numbers * r;
     const int number = rest / r, n = kv * r + (rest - number * r);
     const int seq = sequence_of(a.b, number, ROWS, 1);
@@ -218,8 +218,6 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
     if (own && lh == 0) a.lse[t * a.b.h + n] = (m_run + __builtin_amdgcn_logf(l)) * LN2;
 }
 
-int64_t window_attention_pieces(int64_t T, int64_t B) { return win::pieces(T, B, win::ROWS, 1); }
-
 template <int D>
 static hipError_t launch_forward_of(const win::FwdArgs& a, hipStream_t st) {
     auto kern = window_attention_forward_kernel<D>;
@@ -235,7 +233,7 @@ hipError_t launch_window_attention_forward(const uint16_t* qkv, uint16_t* o, flo
     win::FwdArgs a;
     a.b = {off, (int)T, (int)B, (int)h, (int)g, (int)window, (int)sinks};
     a.qkv = qkv; a.o = o; a.lse = lse;
-    a.numbers = (int)window_attention_pieces(T, B);
+    a.numbers = (int)win::pieces(T, B, win::ROWS, 1);
     a.total = (int)(a.numbers * h);
     return d == 128 ? launch_forward_of<128>(a, st) : launch_forward_of<64>(a, st);
 }
