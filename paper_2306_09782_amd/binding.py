@@ -407,68 +407,86 @@ def lomo_cross_entropy_mean(logits, targets, loss_scale, loss, dlogits, stats, s
                                                   _ptr(stats), T, V, _stream(stream)))
 
 
-def _expect(t, dtype, shape, name, device=None):
-    """`t` as the C side takes it for granted: its type, its shape (None: any size), dense rows, its device."""
-    if t.dtype != dtype or t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
-        raise LomoError(f"{name}: {str(t.dtype)[6:]} {tuple(t.shape)}, want {str(dtype)[6:]} {shape}")
-    if not t.is_contiguous():
-        raise LomoError(f"{name} is not contiguous")
-    _on_device(t, name, device)
+def _torch():
+    """The module, found once: these calls are short, and an import statement takes a share of them."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _TORCH = torch
+    return _TORCH
 
 
-def _on_device(t, name, device):
-    if device is not None and t.device != device:
-        raise LomoError(f"{name} is on {t.device}, not on {device}")
+_TORCH = None
 
 
-def _current_device(t, name):
-    """The tensors' common device, which has to be the current one: that is where the launches go."""
-    import torch
-    if t.device.type != "cuda" or t.device.index != torch._C._cuda_getDevice():
+def _device(t, name):
+    """Index of the tensors' common device, which has to be the current one: that is where the launches go."""
+    index = t.get_device()
+    if index < 0 or index != _torch()._C._cuda_getDevice():
         raise LomoError(f"{name} is on {t.device}, which is not the current device")
-    return t.device
+    return index
+
+
+def _expect(t, dtype, shape, device, name):
+    """`t` as the C side takes it for granted: its type, its shape, dense rows, its device."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return
+    if t.dtype is not dtype or t.shape != shape:
+        raise LomoError(f"{name}: {str(t.dtype)[6:]} {tuple(t.shape)}, want {str(dtype)[6:]} {tuple(shape)}")
+    raise LomoError(f"{name} is on {t.device}" if t.get_device() != device else f"{name} is not contiguous")
+
+
+def _raw_stream(stream):
+    return _current_stream() if stream is None else stream.cuda_stream
+
+
+def _rows(t, T, width, name):
+    """Row stride of a fp16 tensor [T x at least `width`] with dense rows; a single row has any."""
+    if t.dtype is not _torch().float16 or t.dim() != 2 or t.shape[0] != T or t.shape[1] < width or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise LomoError(f"{name}: {str(t.dtype)[6:]} {tuple(t.shape)}, strides {t.stride()}, want float16 [{T} x at least {width}] with dense rows")
+    return t.stride(0) if T > 1 else width
 
 
 def lomo_rope_axes(x, y, rope_cos, rope_sin, positions, pair_axis, n_heads, head_dim, inverse=False, stream=None):
     """Rows of x and y may be longer than n_heads * head_dim and need not be adjacent; y may be x.  positions [axes x T];
-    pair_axis: the axis of each of the head_dim / 2 pairs (a sequence of int)."""
-    import torch
-    T, device = x.shape[0], _current_device(x, "x")
-    for t, name in ((x, "x"), (y, "y")):
-        if t.dtype != torch.float16 or t.dim() != 2 or t.shape[0] != T or t.shape[1] < n_heads * head_dim or (t.shape[1] > 1 and t.stride(1) != 1):
-            raise LomoError(f"{name}: {str(t.dtype)[6:]} {tuple(t.shape)}, want float16 [{T} x at least {n_heads * head_dim}] with dense rows")
-    _on_device(y, "y", device)
-    _expect(rope_cos, torch.float32, (None, head_dim // 2), "rope_cos", device)
-    _expect(rope_sin, torch.float32, tuple(rope_cos.shape), "rope_sin", device)
-    _expect(positions, torch.int32, (None, T), "positions", device)
-    axes = bytes(pair_axis)
+    pair_axis: the axis of each of the head_dim / 2 pairs (bytes, or any sequence of int)."""
+    torch = _torch()
+    T, device, width = x.shape[0], _device(x, "x"), n_heads * head_dim
+    ldx, ldy = _rows(x, T, width, "x"), _rows(y, T, width, "y")
+    if y.get_device() != device:
+        raise LomoError(f"y is on {y.device}")
+    P, A = (rope_cos.shape[0] if rope_cos.dim() == 2 else 0), (positions.shape[0] if positions.dim() == 2 else 0)
+    _expect(rope_cos, torch.float32, (P, head_dim // 2), device, "rope_cos")
+    _expect(rope_sin, torch.float32, (P, head_dim // 2), device, "rope_sin")
+    _expect(positions, torch.int32, (A, T), device, "positions")
+    axes = pair_axis if isinstance(pair_axis, bytes) else bytes(pair_axis)
     if len(axes) != head_dim // 2:
         raise LomoError(f"pair_axis has {len(axes)} entries, want {head_dim // 2}")
-    ld = lambda t: t.stride(0) if T > 1 else max(t.shape[1] // 8 * 8, n_heads * head_dim)      # torch gives a single row any stride
-    _check(load_library().lomo_rope_axes(_ptr(x), ld(x), _ptr(y), ld(y), _ptr(rope_cos), _ptr(rope_sin), rope_cos.shape[0], _ptr(positions),
-                                         positions.shape[0], axes, T, n_heads, head_dim, 1 if inverse else 0, _stream(stream)))
+    _check(load_library().lomo_rope_axes(x.data_ptr(), ldx, y.data_ptr(), ldy, rope_cos.data_ptr(), rope_sin.data_ptr(), P,
+                                         positions.data_ptr(), A, axes, T, n_heads, head_dim, 1 if inverse else 0, _raw_stream(stream)))
 
 
 def _window_sizes(qkv, o, lse, seq_offsets, n_heads, n_kv_heads):
-    import torch
-    T, device = qkv.shape[0], _current_device(qkv, "qkv")
+    torch = _torch()
+    device = _device(qkv, "qkv")
     if n_heads < 1 or n_kv_heads < 1 or o.dim() != 2 or o.shape[1] % n_heads:
         raise LomoError(f"o: {tuple(o.shape)} for {n_heads} heads, {n_kv_heads} of keys")
-    d = o.shape[1] // n_heads
-    _expect(qkv, torch.float16, (T, (n_heads + 2 * n_kv_heads) * d), "qkv", device)
-    _expect(o, torch.float16, (T, n_heads * d), "o", device)
-    _expect(lse, torch.float32, (T, n_heads), "lse", device)
-    _expect(seq_offsets, torch.int32, (None,), "seq_offsets", device)
-    if seq_offsets.numel() < 1:
+    T, d = qkv.shape[0], o.shape[1] // n_heads
+    _expect(qkv, torch.float16, (T, (n_heads + 2 * n_kv_heads) * d), device, "qkv")
+    _expect(o, torch.float16, (T, n_heads * d), device, "o")
+    _expect(lse, torch.float32, (T, n_heads), device, "lse")
+    n = seq_offsets.numel()
+    _expect(seq_offsets, torch.int32, (n,), device, "seq_offsets")
+    if n < 1:
         raise LomoError("seq_offsets is empty")
-    return T, seq_offsets.numel() - 1, d, device
+    return T, n - 1, d, device
 
 
 def lomo_window_attention_forward(qkv, o, lse, seq_offsets, n_heads, n_kv_heads, window, sinks=0, stream=None):
     """seq_offsets: int32 [number of sequences + 1] on the device."""
     T, B, d, _ = _window_sizes(qkv, o, lse, seq_offsets, n_heads, n_kv_heads)
-    _check(load_library().lomo_window_attention_forward(_ptr(qkv), _ptr(o), _ptr(lse), _ptr(seq_offsets), T, B, n_heads, n_kv_heads, d,
-                                                        window, sinks, _stream(stream)))
+    _check(load_library().lomo_window_attention_forward(qkv.data_ptr(), o.data_ptr(), lse.data_ptr(), seq_offsets.data_ptr(), T, B, n_heads,
+                                                        n_kv_heads, d, window, sinks, _raw_stream(stream)))
 
 
 def lomo_window_attention_workspace_bytes(T: int, B: int, n_heads: int, n_kv_heads: int, head_dim: int, sinks: int = 0) -> int:
@@ -476,42 +494,45 @@ def lomo_window_attention_workspace_bytes(T: int, B: int, n_heads: int, n_kv_hea
 
 
 def lomo_window_attention_backward(qkv, o, dO, lse, dqkv, seq_offsets, n_heads, n_kv_heads, window, sinks, ws, stream=None):
-    import torch
+    torch = _torch()
     T, B, d, device = _window_sizes(qkv, o, lse, seq_offsets, n_heads, n_kv_heads)
-    _expect(dO, torch.float16, tuple(o.shape), "dO", device)
-    _expect(dqkv, torch.float16, tuple(qkv.shape), "dqkv", device)
-    _on_device(ws, "ws", device)
-    _check(load_library().lomo_window_attention_backward(_ptr(qkv), _ptr(o), _ptr(dO), _ptr(lse), _ptr(dqkv), _ptr(seq_offsets), T, B,
-                                                         n_heads, n_kv_heads, d, window, sinks, _ptr(ws), _nbytes(ws), _stream(stream)))
+    _expect(dO, torch.float16, o.shape, device, "dO")
+    _expect(dqkv, torch.float16, qkv.shape, device, "dqkv")
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise LomoError(f"ws is on {ws.device}, or not contiguous")
+    _check(load_library().lomo_window_attention_backward(qkv.data_ptr(), o.data_ptr(), dO.data_ptr(), lse.data_ptr(), dqkv.data_ptr(),
+                                                         seq_offsets.data_ptr(), T, B, n_heads, n_kv_heads, d, window, sinks, ws.data_ptr(),
+                                                         _nbytes(ws), _raw_stream(stream)))
 
 
 def _distill_sizes(logits, teacher_ids, teacher_logits, targets, loss, dlogits):
-    import torch
-    device = _current_device(logits, "logits")
-    _expect(logits, torch.float16, (None, None), "logits")
-    T, V = logits.shape
-    _expect(teacher_ids, torch.int32, (T, None), "teacher_ids", device)
-    K = teacher_ids.shape[1]
-    _expect(teacher_logits, torch.float16, (T, K), "teacher_logits", device)
-    _expect(targets, torch.int32, (T,), "targets", device)
-    _expect(loss, torch.float32, (T,), "loss", device)
-    _expect(dlogits, torch.float16, (T, V), "dlogits", device)
+    torch = _torch()
+    device = _device(logits, "logits")
+    if logits.dim() != 2 or teacher_ids.dim() != 2:
+        raise LomoError(f"logits {tuple(logits.shape)} and teacher_ids {tuple(teacher_ids.shape)}, want [tokens x vocabulary] and [tokens x kept]")
+    (T, V), K = logits.shape, teacher_ids.shape[1]
+    _expect(logits, torch.float16, (T, V), device, "logits")
+    _expect(teacher_ids, torch.int32, (T, K), device, "teacher_ids")
+    _expect(teacher_logits, torch.float16, (T, K), device, "teacher_logits")
+    _expect(targets, torch.int32, (T,), device, "targets")
+    _expect(loss, torch.float32, (T,), device, "loss")
+    _expect(dlogits, torch.float16, (T, V), device, "dlogits")
     return T, V, K, device
 
 
 def lomo_distill(logits, teacher_ids, teacher_logits, targets, grad_scale, temperature, soft_weight, loss, dlogits, stream=None):
     T, V, K, _ = _distill_sizes(logits, teacher_ids, teacher_logits, targets, loss, dlogits)
-    _check(load_library().lomo_distill(_ptr(logits), _ptr(teacher_ids), _ptr(teacher_logits), _ptr(targets), grad_scale, temperature,
-                                       soft_weight, _ptr(loss), _ptr(dlogits), T, V, K, _stream(stream)))
+    _check(load_library().lomo_distill(logits.data_ptr(), teacher_ids.data_ptr(), teacher_logits.data_ptr(), targets.data_ptr(), grad_scale,
+                                       temperature, soft_weight, loss.data_ptr(), dlogits.data_ptr(), T, V, K, _raw_stream(stream)))
 
 
 def lomo_distill_mean(logits, teacher_ids, teacher_logits, targets, loss_scale, temperature, soft_weight, loss, dlogits, stats, stream=None):
     """stats: device float64[3]; receives (mean loss over the counted targets, their number, scratch)."""
-    import torch
     T, V, K, device = _distill_sizes(logits, teacher_ids, teacher_logits, targets, loss, dlogits)
-    _expect(stats, torch.float64, (3,), "stats", device)
-    _check(load_library().lomo_distill_mean(_ptr(logits), _ptr(teacher_ids), _ptr(teacher_logits), _ptr(targets), loss_scale, temperature,
-                                            soft_weight, _ptr(loss), _ptr(dlogits), _ptr(stats), T, V, K, _stream(stream)))
+    _expect(stats, _torch().float64, (3,), device, "stats")
+    _check(load_library().lomo_distill_mean(logits.data_ptr(), teacher_ids.data_ptr(), teacher_logits.data_ptr(), targets.data_ptr(), loss_scale,
+                                            temperature, soft_weight, loss.data_ptr(), dlogits.data_ptr(), stats.data_ptr(), T, V, K,
+                                            _raw_stream(stream)))
 
 
 PROBE_OPERAND_BYTES = 16 * 64 * 16

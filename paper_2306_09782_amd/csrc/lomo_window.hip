@@ -216,10 +216,10 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
     const int place = place_of_block(a.total_q, blockIdx.x), r = a.b.h / a.b.g;
     const int kv = place / (a.numbers_q * r), rest = place - kv * a.numbers_q * r;
     const int number = rest / r, n = kv * r + (rest - number * r);
-    const int seq = sequence_of(a.b, number, ROWS, 1);
+    Rows s;
+    const int seq = sequence_of(a.b, number, ROWS, 1, s);
     if (seq < 0) return;
-    const Rows s = rows_of(a.b, seq);
-    const int nb = (s.len + ROWS - 1) / ROWS, at = number - first_piece(a.b, seq, ROWS, 1);
+    const int nb = (s.len + ROWS - 1) / ROWS, at = number - first_piece(s.start, seq, ROWS, 1);
     if (at >= nb) return;
     const int q0 = (nb - 1 - at) * ROWS, qw = q0 + 32 * wave;      // the longest walks first
     const bool active = qw < s.len;
@@ -349,10 +349,9 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
     if ((int)blockIdx.x < a.far) {
         const int number = blockIdx.x / a.b.g;
         kv = blockIdx.x - number * a.b.g;
-        seq = sequence_of(a.b, number, FAR_ROWS, 2);
+        seq = sequence_of(a.b, number, FAR_ROWS, 2, s);
         if (seq < 0) return;
-        s = rows_of(a.b, seq);
-        const int piece = number - first_piece(a.b, seq, FAR_ROWS, 2) - 1;      // the first number is for the sums of the block of keys
+        const int piece = number - first_piece(s.start, seq, FAR_ROWS, 2) - 1;      // the first number is for the sums of the block of keys
         if (piece < 0 || !has_far(a.b, s.len)) return;
         const int from = max((int64_t)piece * FAR_ROWS, (int64_t)a.b.window), to = min((int64_t)s.len, (int64_t)(piece + 1) * FAR_ROWS);
         if (from >= to) return;
@@ -367,16 +366,15 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
         const int place = place_of_block(a.total_k, (int)blockIdx.x - a.far);
         kv = place / a.numbers_k;
         const int number = place - kv * a.numbers_k;
-        seq = sequence_of(a.b, number, BLK, 1);
+        seq = sequence_of(a.b, number, BLK, 1, s);
         if (seq < 0) return;
-        s = rows_of(a.b, seq);
-        k0 = (number - first_piece(a.b, seq, BLK, 1)) * BLK;      // the longest walks first
+        k0 = (number - first_piece(s.start, seq, BLK, 1)) * BLK;      // the longest walks first
         if (k0 >= s.len) return;
         near = 0;
         reach = (uint32_t)a.b.window;
         first = k0 / BLK;
         last = (int)min((int64_t)s.len - 1, (int64_t)k0 + BLK - 2 + a.b.window) / BLK;
-        if (k0 == 0 && has_far(a.b, s.len)) slot = slot_at<D>(a, first_piece(a.b, seq, FAR_ROWS, 2), kv);
+        if (k0 == 0 && has_far(a.b, s.len)) slot = slot_at<D>(a, first_piece(s.start, seq, FAR_ROWS, 2), kv);
     }
     const int kw = k0 + 32 * (wave & 1), key = kw + l32;
     const bool active = kw < s.len && (near == 0 || kw < a.b.sinks);
@@ -485,7 +483,7 @@ __global__ __launch_bounds__(256) void window_attention_sinks_kernel(win::BwdArg
     const int i = (blockIdx.x - pair * per) * 256 + threadIdx.x;
     const int which = i / (a.b.sinks * D), row = (i - which * a.b.sinks * D) / D, c = i % D;
     if (!has_far(a.b, s.len) || which > 1 || row >= s.len) return;
-    const int base = first_piece(a.b, seq, FAR_ROWS, 2);
+    const int base = first_piece(s.start, seq, FAR_ROWS, 2);
     const int from = a.b.window / FAR_ROWS, to = (s.len - 1) / FAR_ROWS;
     const int64_t step = (int64_t)a.b.g * 2 * a.b.sinks * D;
     const float* p = slot_at<D>(a, base, kv) + ((int64_t)which * a.b.sinks + row) * D + c;

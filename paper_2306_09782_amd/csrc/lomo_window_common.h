@@ -46,21 +46,27 @@ __device__ __forceinline__ Rows rows_of(const Batch& a, int b) {
 }
 
 // Pieces of `unit` rows are numbered through all sequences without a table: those of sequence b begin at
-// floor(off[b] / unit) + more * b, which leaves room for ceil(length / unit) + more - 1 of them.  The sequence that number i falls in, by a
-// 64-way search of the wave, or -1.
-__device__ __forceinline__ int first_piece(const Batch& a, int b, int unit, int more) { return clamped(a, b) / unit + more * b; }
-__device__ __forceinline__ int sequence_of(const Batch& a, int i, int unit, int more) {
+// floor(off[b] / unit) + more * b, which leaves room for ceil(length / unit) + more - 1 of them.
+__device__ __forceinline__ int first_piece(int start, int b, int unit, int more) { return start / unit + more * b; }
+// The sequence that number i falls in, by a 64-way search of the wave, and its rows; -1: none.  The last round has the rows at hand.
+__device__ __forceinline__ int sequence_of(const Batch& a, int i, int unit, int more, Rows& rows) {
     const int lane = threadIdx.x & 63;
     int lo = 0, n = a.B;
     while (true) {
-        const int step = (n + 63) >> 6;
-        const bool in = lane * step < n;
-        const bool at_or_before = in && first_piece(a, lo + (in ? lane * step : 0), unit, more) <= i;
-        const int count = __popcll(__ballot(at_or_before));
+        const int step = (n + 63) >> 6, at = lo + min(lane * step, n);      // at most off's last
+        const int start = clamped(a, at);
+        const int count = __popcll(__ballot(lane * step < n && first_piece(start, at, unit, more) <= i));
         if (count == 0) return -1;
-        lo += (count - 1) * step;
-        n = min(step, n - (count - 1) * step);
-        if (step == 1) return __builtin_amdgcn_readfirstlane(lo);
+        if (step > 1) {
+            lo += (count - 1) * step;
+            n = min(step, n - (count - 1) * step);
+            continue;
+        }
+        const int seq = __builtin_amdgcn_readfirstlane(lo + count - 1);
+        rows.start = __builtin_amdgcn_readlane(start, count - 1);
+        const int end = count < 64 ? __builtin_amdgcn_readlane(start, count & 63) : clamped(a, seq + 1);
+        rows.len = max(__builtin_amdgcn_readfirstlane(end) - rows.start, 0);
+        return seq;
     }
 }
 inline int64_t pieces(int64_t T, int64_t B, int64_t unit, int64_t more) { return T / unit + more * B; }

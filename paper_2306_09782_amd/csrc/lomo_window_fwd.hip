@@ -42,10 +42,10 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
     const int place = place_of_block(a.total, blockIdx.x), r = a.b.h / a.b.g;
     const int kv = place / (a.numbers * r), rest = place - kv * a.numbers * r;
     const int number = rest / r, n = kv * r + (rest - number * r);
-    const int seq = sequence_of(a.b, number, ROWS, 1);
+    Rows s;
+    const int seq = sequence_of(a.b, number, ROWS, 1, s);
     if (seq < 0) return;
-    const Rows s = rows_of(a.b, seq);
-    const int nb = (s.len + ROWS - 1) / ROWS, at = number - first_piece(a.b, seq, ROWS, 1);
+    const int nb = (s.len + ROWS - 1) / ROWS, at = number - first_piece(s.start, seq, ROWS, 1);
     if (at >= nb) return;
     const int q0 = (nb - 1 - at) * ROWS, qw = q0 + 32 * wave;      // the longest walks first
     const bool active = qw < s.len;
