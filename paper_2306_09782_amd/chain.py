@@ -13,7 +13,7 @@ input has been taken from the old value.  Nothing waits on the host.
 """
 from __future__ import annotations
 
-from typing import Dict
+from typing import Dict, NamedTuple
 
 import torch
 
@@ -155,18 +155,87 @@ class LomoMlpBlock:
         return self.state.result()
 
 
+class PackedAttention:
+    """Attention over sequences of any length packed into the rows of a batch, in place of equal sequences of a multiple of 64
+    tokens: heads of 64 or 128 columns that share n_kv_heads heads of keys and values, a window, sinks, and rotary positions on
+    several axes.  One object serves all layers of a step.
+
+    W_qkv is then [(n_heads + 2 n_kv_heads) head_dim x H], with n_heads * head_dim = H; rope_cos and rope_sin are tables
+    [positions x head_dim / 2].  window=None: no limit.  pair_axis: the axis of each of the head_dim / 2 pairs (None: one axis).
+
+    set_batch(lengths, positions) before a step: lengths on the host, at most max_sequences of them, their sum at most T; positions
+    int32 [axes x T] on the device (None: each token's place in its sequence, on every axis).  Rows behind the last sequence are padding:
+    their targets have to be outside the vocabulary, then they add nothing to any gradient."""
+
+    def __init__(self, device, T: int, n_heads: int, n_kv_heads: int, head_dim: int, window: int = None, sinks: int = 0,
+                 max_sequences: int = 64, pair_axis=None):
+        self.device = torch.device(device)
+        self.T, self.n_heads, self.n_kv_heads, self.head_dim = T, n_heads, n_kv_heads, head_dim
+        self.window, self.sinks = (max(T, 1) if window is None else window), sinks
+        self.pair_axis = bytes(head_dim // 2) if pair_axis is None else bytes(pair_axis)
+        self.qkv_width = (n_heads + 2 * n_kv_heads) * head_dim
+        nbytes = B.lomo_window_attention_workspace_bytes(T, max_sequences, n_heads, n_kv_heads, head_dim, sinks)
+        if T > 0 and max_sequences > 0 and nbytes == 0:
+            raise B.LomoError(f"no attention for {n_heads} / {n_kv_heads} heads of {head_dim}, {sinks} sinks")
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self.offsets = torch.zeros(max_sequences + 1, dtype=torch.int32, device=self.device)
+        self.positions = torch.zeros(1 + max(self.pair_axis, default=0), T, dtype=torch.int32, device=self.device)
+        self.rows = 0
+
+    def set_batch(self, lengths, positions=None) -> None:
+        lengths = [int(n) for n in lengths]
+        if min(lengths, default=0) < 0 or sum(lengths) > self.T or len(lengths) >= self.offsets.numel():
+            raise B.LomoError(f"{len(lengths)} sequences of {sum(lengths)} tokens, room for {self.offsets.numel() - 1} of {self.T}")
+        at, place = [0], torch.zeros(self.T, dtype=torch.int32)
+        for n in lengths:
+            place[at[-1]:at[-1] + n] = torch.arange(n, dtype=torch.int32)
+            at.append(at[-1] + n)
+        self.rows = at[-1]
+        # the sequences that are not there are empty ones: the buffers, and what a captured step reads, stay the same
+        self.offsets.copy_(torch.tensor(at + [self.rows] * (self.offsets.numel() - len(at)), dtype=torch.int32))
+        if positions is None:
+            positions = place.expand_as(self.positions)
+        if tuple(positions.shape) != tuple(self.positions.shape):
+            raise B.LomoError(f"positions {tuple(positions.shape)}, want {tuple(self.positions.shape)}")
+        self.positions.copy_(positions)
+
+    def forward(self, qkv, rope_cos, rope_sin, o, lse, stream=None) -> None:
+        """qkv [T x qkv_width] as the projection leaves it: its q and k are turned in place."""
+        B.lomo_rope_axes(qkv, qkv, rope_cos, rope_sin, self.positions, self.pair_axis, self.n_heads + self.n_kv_heads, self.head_dim,
+                         stream=stream)
+        B.lomo_window_attention_forward(qkv, o, lse, self.offsets, self.n_heads, self.n_kv_heads, self.window, self.sinks, stream)
+        self._clear_padding(o, stream)
+
+    def backward(self, qkv, o, dO, lse, rope_cos, rope_sin, dqkv, stream=None) -> None:
+        """dqkv: the gradient of the projection's output."""
+        B.lomo_window_attention_backward(qkv, o, dO, lse, dqkv, self.offsets, self.n_heads, self.n_kv_heads, self.window, self.sinks,
+                                         self.ws, stream)
+        self._clear_padding(dqkv, stream)
+        B.lomo_rope_axes(dqkv, dqkv, rope_cos, rope_sin, self.positions, self.pair_axis, self.n_heads + self.n_kv_heads, self.head_dim,
+                         inverse=True, stream=stream)
+
+    def _clear_padding(self, x, stream):
+        """The kernels leave rows of no sequence as they are; the products that follow take them all."""
+        if self.rows < self.T:
+            with B.on_stream(stream):
+                x[self.rows:].zero_()
+
+
 class LomoAttentionBlock:
     """Hand-on buffers of the attention block: do [T x H], [dq|dk|dv] [T x 3H], dxn [T x H], delta [T x heads].
-    `saved`: o, xn, xhat [T x H], rstd [T] fp32, qkv [T x 3H] (rotated q and k, v), lse [T x heads] fp32."""
+    `saved`: o, xn, xhat [T x H], rstd [T] fp32, qkv [T x 3H] (rotated q and k, v), lse [T x heads] fp32.
+    With `packed` (PackedAttention) qkv and its gradient are packed.qkv_width wide."""
 
     def __init__(self, device, batch: int, seq: int, H: int, n_heads: int, state: StepState = None, slot0: int = 0,
-                 share=None):
+                 share=None, packed: PackedAttention = None):
         self.device = torch.device(device)
         T = batch * seq
-        self.batch, self.seq, self.n_heads = batch, seq, n_heads
+        self.batch, self.seq, self.n_heads, self.packed = batch, seq, n_heads, packed
+        if packed is not None and (packed.T, packed.n_heads, packed.n_heads * packed.head_dim) != (T, n_heads, H):
+            raise B.LomoError(f"attention of {packed.T} rows, {packed.n_heads} heads of {packed.head_dim}, want {T} rows, {n_heads} heads, {H} columns")
         f16 = dict(dtype=torch.float16, device=self.device)
         self.do = share.do if share is not None else torch.empty(T, H, **f16)
-        self.dqkv = share.dqkv if share is not None else torch.empty(T, 3 * H, **f16)
+        self.dqkv = share.dqkv if share is not None else torch.empty(T, 3 * H if packed is None else packed.qkv_width, **f16)
         self.dxn = share.dxn if share is not None else torch.empty(T, H, **f16)
         self.delta = share.delta if share is not None else torch.empty(T * n_heads, dtype=torch.float32, device=self.device)
         self.state = state if state is not None else StepState(self.device, 3, T, H)
@@ -186,8 +255,11 @@ class LomoAttentionBlock:
         out, qkv, gain = self._tensor_lists(dy, saved, w, W_qkv, W_o)
         st, k = self.state, self.slot0
         _linear(st, k, saved["o"], dy, W_o, self.do, out, update, stream)
-        B.lomo_attention_backward(saved["qkv"], saved["o"], self.do, saved["lse"], rope_cos, rope_sin, self.delta,
-                                  self.dqkv, self.batch, self.seq, self.n_heads, stream)
+        if self.packed is not None:
+            self.packed.backward(saved["qkv"], saved["o"], self.do, saved["lse"], rope_cos, rope_sin, self.dqkv, stream)
+        else:
+            B.lomo_attention_backward(saved["qkv"], saved["o"], self.do, saved["lse"], rope_cos, rope_sin, self.delta,
+                                      self.dqkv, self.batch, self.seq, self.n_heads, stream)
         _linear(st, k + 1, saved["xn"], self.dqkv, W_qkv, self.dxn, qkv, update, stream)
         B.lomo_rmsnorm_backward(self.dxn, saved["xhat"], saved["rstd"], w, dy, dh, stream)
         _gain(st, k + 2, saved["xhat"], self.dxn, w, gain, update, stream)
@@ -207,12 +279,12 @@ class LomoAttentionBlock:
 class LomoDecoderLayer:
     """Both blocks under one step: flags in backward order W_d, W_gu, w2, W_o, W_qkv, w1."""
 
-    def __init__(self, device, batch: int, seq: int, H: int, F: int, n_heads: int):
+    def __init__(self, device, batch: int, seq: int, H: int, F: int, n_heads: int, packed: PackedAttention = None):
         self.device = torch.device(device)
         T = batch * seq
         self.state = StepState(self.device, 6, T, H)
         self.mlp = LomoMlpBlock(self.device, T, H, F, self.state, 0)
-        self.attn = LomoAttentionBlock(self.device, batch, seq, H, n_heads, self.state, 3)
+        self.attn = LomoAttentionBlock(self.device, batch, seq, H, n_heads, self.state, 3, packed=packed)
         self.dh_mid = torch.empty(T, H, dtype=torch.float16, device=self.device)
 
     def _walk(self, dy, saved_attn, saved_mlp, p, rope_cos, rope_sin, dh, update, stream):
@@ -248,7 +320,8 @@ class LomoModelChain:
     out bit-identical to the re-walked step, since the hand-ons of both passes are the same bits."""
 
     def __init__(self, device, batch: int, seq: int, H: int, F: int, n_heads: int, n_layers: int,
-                 share_buffers: bool = True, keep_handons: bool = False, overlap_norm_pass: bool = False):
+                 share_buffers: bool = True, keep_handons: bool = False, overlap_norm_pass: bool = False,
+                 packed: PackedAttention = None):
         self.device = torch.device(device)
         T = batch * seq
         self.n_layers = n_layers
@@ -265,7 +338,7 @@ class LomoModelChain:
             first = k == 0 or not share_buffers
             self.mlp.append(LomoMlpBlock(self.device, T, H, F, self.state, slot, share=None if first else self.mlp[0]))
             self.attn.append(LomoAttentionBlock(self.device, batch, seq, H, n_heads, self.state, slot + 3,
-                                                share=None if first else self.attn[0]))
+                                                share=None if first else self.attn[0], packed=packed))
         f16 = dict(dtype=torch.float16, device=self.device)
         self.dxn_f = torch.empty(T, H, **f16)
         n_dy = 2 if share_buffers else n_layers + 1
@@ -379,7 +452,8 @@ class LomoGroupedNormChain:
     Overflow: a group's step flag is the OR of its tensors' flags and of the previous group's step flag, so a group
     with a non-finite gradient and every group after it keep their bits; groups above have been updated already."""
 
-    def __init__(self, device, batch: int, seq: int, H: int, F: int, n_heads: int, n_layers: int, layers_per_group: int = 1):
+    def __init__(self, device, batch: int, seq: int, H: int, F: int, n_heads: int, n_layers: int, layers_per_group: int = 1,
+                 packed: PackedAttention = None):
         self.device = torch.device(device)
         T = batch * seq
         per = max(1, min(layers_per_group, n_layers))
@@ -407,7 +481,7 @@ class LomoGroupedNormChain:
             share = j < len(self.mlp) and k >= per          # later groups reuse the first group's buffers
             self.mlp.append(LomoMlpBlock(self.device, T, H, F, self.groups[g], 6 * j, share=self.mlp[j] if share else None))
             self.attn.append(LomoAttentionBlock(self.device, batch, seq, H, n_heads, self.groups[g], 6 * j + 3,
-                                                share=self.attn[j] if share else None))
+                                                share=self.attn[j] if share else None, packed=packed))
         f16 = dict(dtype=torch.float16, device=self.device)
         self.dxn_f = torch.empty(T, H, **f16)
         self.dy = [torch.empty(T, H, **f16) for _ in range(per + 1)]
@@ -499,31 +573,43 @@ class LayerActivations:
     (rotated q | rotated k | v), o, lse}, feed-forward block {xhat, rstd, xn, gate_up, a}, and y1, the attention
     block's output (the feed-forward block's input)."""
 
-    def __init__(self, device, T: int, H: int, F: int, n_heads: int):
+    def __init__(self, device, T: int, H: int, F: int, n_heads: int, qkv_width: int = None):
         f16 = dict(dtype=torch.float16, device=device)
         f32 = dict(dtype=torch.float32, device=device)
         self.attn = {"xhat": torch.empty(T, H, **f16), "rstd": torch.empty(T, **f32), "xn": torch.empty(T, H, **f16),
-                     "qkv": torch.empty(T, 3 * H, **f16), "o": torch.empty(T, H, **f16), "lse": torch.empty(T, n_heads, **f32)}
+                     "qkv": torch.empty(T, 3 * H if qkv_width is None else qkv_width, **f16), "o": torch.empty(T, H, **f16), "lse": torch.empty(T, n_heads, **f32)}
         self.mlp = {"xhat": torch.empty(T, H, **f16), "rstd": torch.empty(T, **f32), "xn": torch.empty(T, H, **f16),
                     "gate_up": torch.empty(T, 2 * F, **f16), "a": torch.empty(T, F, **f16)}
         self.y1 = torch.empty(T, H, **f16)
 
 
 def layer_forward(h, p: Dict, act: LayerActivations, rope_cos, rope_sin, batch: int, seq: int, n_heads: int, eps: float,
-                  h_next=None, stream=None) -> None:
+                  h_next=None, stream=None, packed: PackedAttention = None) -> None:
     """Forward of one decoder layer from its input h into `act`; with h_next also the layer output
-    h_next = y1 + a W_d^T (a recomputation before the backward walk does not need it)."""
+    h_next = y1 + a W_d^T (a recomputation before the backward walk does not need it).  `packed`: its attention instead of
+    that over `batch` sequences of `seq` tokens."""
     sa, sm = act.attn, act.mlp
     B.lomo_rmsnorm_forward(h, p["w1"], eps, sa["xhat"], sa["rstd"], sa["xn"], stream)
     B.lomo_linear_forward(sa["xn"], p["W_qkv"], sa["qkv"], False, stream)
-    B.lomo_rope_forward(sa["qkv"], rope_cos, rope_sin, seq, n_heads, stream)
-    B.lomo_attention_forward(sa["qkv"], sa["o"], sa["lse"], batch, seq, n_heads, stream)
+    if packed is not None:
+        packed.forward(sa["qkv"], rope_cos, rope_sin, sa["o"], sa["lse"], stream)
+    else:
+        B.lomo_rope_forward(sa["qkv"], rope_cos, rope_sin, seq, n_heads, stream)
+        B.lomo_attention_forward(sa["qkv"], sa["o"], sa["lse"], batch, seq, n_heads, stream)
     B.lomo_linear_forward_residual(sa["o"], p["W_o"], h, act.y1, stream)           # y1 = h + o W_o^T, one rounding
     B.lomo_rmsnorm_forward(act.y1, p["w2"], eps, sm["xhat"], sm["rstd"], sm["xn"], stream)
     B.lomo_linear_forward(sm["xn"], p["W_gu"], sm["gate_up"], False, stream)
     B.lomo_swiglu_forward(sm["gate_up"], sm["a"], stream)
     if h_next is not None:
         B.lomo_linear_forward_residual(sm["a"], p["W_d"], act.y1, h_next, stream)
+
+
+class Teacher(NamedTuple):
+    """What a step learns from besides its targets: a teacher's top logits, [T x K] (see lomo_distill)."""
+    ids: torch.Tensor            # int32
+    logits: torch.Tensor         # fp16
+    temperature: float = 2.0
+    soft_weight: float = 0.5
 
 
 class LomoFineTuneStep:
@@ -538,54 +624,61 @@ class LomoFineTuneStep:
     checkpoint=False keeps every layer's activations from the forward pass, so nothing is recomputed;
     keep_handons=True (global norm, needs checkpoint=False) also keeps pass 1's hand-on gradients, so pass 2 is
     one grouped fused-update launch over the whole model.  Neither changes a bit of the result.
-    overlap_norm_pass=True (with keep_handons) runs pass 1's norm contractions on a second stream beside the walk."""
+    overlap_norm_pass=True (with keep_handons) runs pass 1's norm contractions on a second stream beside the walk.
+
+    packed (PackedAttention) has the attention of every layer work on packed sequences, with its head layout, window, sinks and
+    positions, in place of `batch` sequences of `seq` tokens; a step with a `teacher` distils from its top logits."""
 
     def __init__(self, device, batch: int, seq: int, H: int, F: int, n_heads: int, n_layers: int, V: int,
                  eps: float = 1e-5, norm: str = "global", layers_per_group: int = 1, checkpoint: bool = True,
-                 keep_handons: bool = False, overlap_norm_pass: bool = False):
+                 keep_handons: bool = False, overlap_norm_pass: bool = False, packed: PackedAttention = None):
         assert norm in ("global", "grouped")
         assert not keep_handons or (norm == "global" and not checkpoint), "kept hand-ons: global norm, no checkpointing"
         self.device = torch.device(device)
         T = batch * seq
         self.batch, self.seq, self.n_heads, self.n_layers, self.eps = batch, seq, n_heads, n_layers, eps
-        self.checkpoint = checkpoint
+        self.checkpoint, self.packed = checkpoint, packed
         f16 = dict(dtype=torch.float16, device=self.device)
         self.ckpt = [torch.empty(T, H, **f16) for _ in range(n_layers + 1)]
         per = layers_per_group if norm == "grouped" else 1
         n_sets = max(1, min(per, n_layers)) if checkpoint else n_layers
-        self.acts = [LayerActivations(self.device, T, H, F, n_heads) for _ in range(n_sets)]
+        self.acts = [LayerActivations(self.device, T, H, F, n_heads, packed.qkv_width if packed is not None else None) for _ in range(n_sets)]
         self.final = {"xhat": torch.empty(T, H, **f16), "rstd": torch.empty(T, dtype=torch.float32, device=self.device),
                       "xn": torch.empty(T, H, **f16)}
         self.logits = torch.empty(T, V, **f16)           # overwritten by its own gradient
         self.token_loss = torch.empty(T, dtype=torch.float32, device=self.device)
         self.loss_stats = torch.zeros(3, dtype=torch.float64, device=self.device)     # mean loss, counted targets, scratch
         if norm == "grouped":
-            self.chain = LomoGroupedNormChain(self.device, batch, seq, H, F, n_heads, n_layers, layers_per_group=per)
+            self.chain = LomoGroupedNormChain(self.device, batch, seq, H, F, n_heads, n_layers, layers_per_group=per, packed=packed)
         else:
             self.chain = LomoModelChain(self.device, batch, seq, H, F, n_heads, n_layers, keep_handons=keep_handons,
-                                        overlap_norm_pass=overlap_norm_pass)
+                                        overlap_norm_pass=overlap_norm_pass, packed=packed)
         # walk index k = n_layers - 1 - layer index; the layers of one group use different activation sets
         self.saved = {"layers": [(self._act(li).attn, self._act(li).mlp) for li in range(n_layers)], "final": self.final}
 
     def _act(self, li: int) -> LayerActivations:
         return self.acts[(self.n_layers - 1 - li) % len(self.acts)]
 
-    def forward(self, ids, targets, loss_scale: float, m: Dict, rope_cos, rope_sin, stream=None) -> None:
+    def forward(self, ids, targets, loss_scale: float, m: Dict, rope_cos, rope_sin, stream=None, teacher: Teacher = None) -> None:
         """Checkpoints, final norm, logits, token losses, and the scaled loss gradient in place of the logits."""
         B.lomo_embedding_forward(ids, m["W_emb"], self.ckpt[0], stream)
         for li, p in enumerate(m["layers"]):
             layer_forward(self.ckpt[li], p, self._act(li), rope_cos, rope_sin, self.batch, self.seq, self.n_heads, self.eps,
-                          self.ckpt[li + 1], stream)
+                          self.ckpt[li + 1], stream, self.packed)
         f = self.final
         B.lomo_rmsnorm_forward(self.ckpt[self.n_layers], m["w_f"], self.eps, f["xhat"], f["rstd"], f["xn"], stream)
         B.lomo_linear_forward(f["xn"], m["W_lm"], self.logits, False, stream)
-        B.lomo_cross_entropy_mean(self.logits, targets, loss_scale, self.token_loss, self.logits, self.loss_stats, stream)
+        if teacher is not None:
+            B.lomo_distill_mean(self.logits, teacher.ids, teacher.logits, targets, loss_scale, teacher.temperature, teacher.soft_weight,
+                                self.token_loss, self.logits, self.loss_stats, stream)
+        else:
+            B.lomo_cross_entropy_mean(self.logits, targets, loss_scale, self.token_loss, self.logits, self.loss_stats, stream)
 
     def step(self, ids, targets, m: Dict, rope_cos, rope_sin, lr: float, loss_scale: float,
-             max_norm: float = 1.0, eps_clip: float = 1e-6, stream=None) -> None:
+             max_norm: float = 1.0, eps_clip: float = 1e-6, stream=None, teacher: Teacher = None) -> None:
         """m as for LomoModelChain, updated in place.  targets [T] int32 (outside [0, V): not counted); the mean loss's
         denominator, the number of counted targets, is taken on the device."""
-        self.forward(ids, targets, loss_scale, m, rope_cos, rope_sin, stream)
+        self.forward(ids, targets, loss_scale, m, rope_cos, rope_sin, stream, teacher)
         fresh = [self.n_layers - 1]          # the forward pass has just left the last layer's activations in place
 
         def recompute(li, k):
@@ -593,7 +686,7 @@ class LomoFineTuneStep:
                 fresh.clear()
                 return
             layer_forward(self.ckpt[li], m["layers"][li], self._act(li), rope_cos, rope_sin, self.batch, self.seq,
-                          self.n_heads, self.eps, None, stream)
+                          self.n_heads, self.eps, None, stream, self.packed)
 
         self.chain.step(ids, self.logits, self.saved, m, rope_cos, rope_sin, lr, loss_scale, max_norm, eps_clip, stream,
                         before_layer=recompute if self.checkpoint else None)
@@ -616,9 +709,9 @@ class LomoTrainer:
         self.step, self.lr, self.loss_scale, self.growth_interval = step, lr, float(loss_scale), growth_interval
         self.max_norm, self.eps_clip, self.clean_steps = max_norm, eps_clip, 0
 
-    def train_step(self, ids, targets, m: Dict, rope_cos, rope_sin, stream=None) -> Dict:
+    def train_step(self, ids, targets, m: Dict, rope_cos, rope_sin, stream=None, teacher: Teacher = None) -> Dict:
         used = self.loss_scale
-        self.step.step(ids, targets, m, rope_cos, rope_sin, self.lr, used, self.max_norm, self.eps_clip, stream)
+        self.step.step(ids, targets, m, rope_cos, rope_sin, self.lr, used, self.max_norm, self.eps_clip, stream, teacher)
         if stream is None:
             torch.cuda.synchronize(self.step.device)
         else:
