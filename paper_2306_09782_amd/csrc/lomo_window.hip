@@ -170,27 +170,35 @@ constexpr int STAT_BYTES = 2 * 2 * BLK * 4;      // lse and delta of the queries
 template <int D>
 constexpr int KEY_LDS_BYTES = DQ_LDS_BYTES<D> + STAT_BYTES + attn::XCH_BYTES;
 
-// The moving pairs of the kernels that own keys: q and do of 64 queries of a head, and their lse and delta.  Rows behind the sequence are zeros with
+// The moving pairs of the kernel that owns keys: q and do of 64 queries of a head, and their lse and delta.  Rows behind the sequence are zeros with
 // an lse of infinity: their probabilities are 0.
-template <int D, int WAVES>
+template <int D>
 struct QueryTiles {
     const BwdArgs& a;
     Rows s;
-    int64_t ld, ldo;
     TileLoad<D> load_q, load_do;
+    const uint16_t *q, *dO;      // of the sequence's first row, head 0
+    const float* stat0;          // lse (wave 0) or delta (wave 1), likewise
     uint32_t lds0;
     float* stats;
     int wave, lane;
     float stat = 0.f;
     __device__ __forceinline__ QueryTiles(const BwdArgs& a, const Rows& s, uint32_t lds0, float* stats)
-        : a(a), s(s), ld((int64_t)(a.b.h + 2 * a.b.g) * D), ldo((int64_t)a.b.h * D), load_q(ld), load_do(ldo), lds0(lds0), stats(stats),
-          wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63) {}
+        : a(a), s(s), load_q((int64_t)(a.b.h + 2 * a.b.g) * D), load_do((int64_t)a.b.h * D),
+          q(a.qkv + (int64_t)s.start * ((a.b.h + 2 * a.b.g) * D)), dO(a.dO + (int64_t)s.start * (a.b.h * D)), lds0(lds0), stats(stats),
+          wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63) {
+        stat0 = (wave == 0 ? a.lse : a.delta) + (int64_t)s.start * a.b.h;
+    }
     __device__ __forceinline__ void fetch(int tile, int n, int buf) {
-        const int64_t t = (int64_t)s.start + tile * BLK;
-        const int rows = s.len - tile * BLK;
-        load_q.template issue<WAVES>(a.qkv + t * ld + (int64_t)n * D, rows, lds0 + (uint32_t)buf * (PAIR<D> * 2u), wave);
-        load_do.template issue<WAVES>(a.dO + t * ldo + (int64_t)n * D, rows, lds0 + (uint32_t)buf * (PAIR<D> * 2u) + TILE<D> * 2u, wave);
-        if (wave < 2) stat = lane < rows ? (wave == 0 ? a.lse : a.delta)[(t + lane) * a.b.h + n] : (wave == 0 ? INFINITY : 0.f);
+        const int left = s.len - tile * BLK;
+        const uint32_t at = lds0 + (uint32_t)buf * (PAIR<D> * 2u);
+        load_q.issue(q + n * D, tile, left, at, wave);
+        load_do.issue(dO + n * D, tile, left, at + TILE<D> * 2u, wave);
+        if (wave < 2) {
+            const float* row = stat0 + (int64_t)tile * (BLK * a.b.h) + n;
+            stat = row[(uint32_t)(min(lane, left - 1) * a.b.h)];
+            if (lane >= left) stat = wave == 0 ? INFINITY : 0.f;
+        }
     }
     // this wave's share of what fetch() brought; a barrier has to follow
     __device__ __forceinline__ void keep_stats(int buf) const {
@@ -237,10 +245,9 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
     const TileLoad<D> load(ld);
     const TileRead<D> rd(lds0);
     auto fetch = [&](int tile, int buf) {
-        const int64_t off = (int64_t)tile * BLK * ld;
-        const int rows = s.len - tile * BLK;
-        load.issue(gk + off, rows, lds0 + (uint32_t)buf * (PAIR<D> * 2u), wave);
-        load.issue(gv + off, rows, lds0 + (uint32_t)buf * (PAIR<D> * 2u) + TILE<D> * 2u, wave);
+        const uint32_t at = lds0 + (uint32_t)buf * (PAIR<D> * 2u);
+        load.issue(gk, tile, s.len - tile * BLK, at, wave);
+        load.issue(gv, tile, s.len - tile * BLK, at + TILE<D> * 2u, wave);
     };
     fetch(tile_at(0), 0);
 
@@ -382,7 +389,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
     const int64_t t = (int64_t)s.start + min(key, s.len - 1);
 
     const int per = last - first + 1, steps = per * r;
-    QueryTiles<D, 4> tiles(a, s, lds0, stats);
+    QueryTiles<D> tiles(a, s, lds0, stats);
     tiles.fetch(first, kv * r, 0);
 
     half8 fk[D / 16], fv[D / 16];

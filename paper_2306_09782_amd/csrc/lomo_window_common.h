@@ -55,7 +55,9 @@ __device__ __forceinline__ int sequence_of(const Batch& a, int i, int unit, int 
     while (true) {
         const int step = (n + 63) >> 6, at = lo + min(lane * step, n);      // at most off's last
         const int start = clamped(a, at);
-        const int count = __popcll(__ballot(lane * step < n && first_piece(start, at, unit, more) <= i));
+        // how many from the first on: also where offsets do not ascend, the last of these begins at or before i
+        const uint64_t before = __ballot(lane * step < n && first_piece(start, at, unit, more) <= i);
+        const int count = ~before == 0 ? 64 : __builtin_ctzll(~before);
         if (count == 0) return -1;
         if (step > 1) {
             lo += (count - 1) * step;
@@ -88,31 +90,50 @@ __device__ __forceinline__ int swz(int r) {
     else return ((r & 2) << 1) | ((r >> 2) & 3);
 }
 
-// Load of a [64 x D] tile whose row 0 is at `base` and of which `rows` (any number) lie in the sequence; the others become zeros: the
-// descriptor ends behind the last one.  Rows are `ld` elements apart, 64 of them less than 4 GiB.
+// Load of [64 x D] tiles of rows `ld` elements apart, 64 of them less than 4 GiB.  A wave fetches 16 neighbouring rows, RPI with an
+// instruction.  The instructions' swizzles differ from that of the first in two chunk bits; their offsets in memory and in LDS share the
+// immediate, so that one value of M0 serves them all.
 template <int D>
 struct TileLoad {
-    static constexpr int RPI = 512 / D;              // rows that an instruction of a wave fetches; a multiple of 16 to a wave
-    uint32_t voff, ld2;
+    static constexpr int RPI = 512 / D, PER = 16 / RPI;
+    uint32_t voff, ld2, step;
     __device__ __forceinline__ TileLoad(int64_t ld) {
         const int lane = threadIdx.x & 63, rr = lane / (D / 8), c = lane % (D / 8);
         ld2 = 2u * (uint32_t)ld;
+        step = RPI * ld2 - 1024u;      // what the scalar offset adds to the immediate
         voff = (uint32_t)rr * ld2 + (uint32_t)((c ^ swz<D>(rr)) * 16);
     }
-    template <int WAVES = 4>
-    __device__ __forceinline__ void issue(const uint16_t* base, int rows, uint32_t tile, int wave) const {
-        constexpr int PER = BLK / RPI / WAVES;
-        const int left = min(rows, BLK) - RPI * PER * wave;      // rows of the sequence among this wave's
-        base += (int64_t)(RPI * PER * wave) * (ld2 / 2);
-        // instruction it fetches rows RPI (PER wave + it) ..; their swizzles differ from those of rows 0 .. in the low two chunk bits
+    // Row 0 of the tile is `tile` tiles from `rows0`, `left` rows of the sequence remain from there (any number); the others become zeros.
+    __device__ __forceinline__ void issue(const uint16_t* rows0, int tile, int left, uint32_t lds, int wave) const {
+        const char* base = reinterpret_cast<const char*>(rows0) + (uint64_t)(uint32_t)tile * (64u * ld2) + (uint64_t)((uint32_t)wave * 16u * ld2);
+        lds += (uint32_t)wave * (16u * D * 2u);
+        uint32_t v[PER];
 #pragma unroll
         for (int it = 0; it < PER; ++it) {
-            const int n = left - RPI * it;
-            const auto srd = dma::make_srd(base, n <= 0 ? 0u : (uint32_t)(min(n, RPI) - 1) * ld2 + 2u * D);
-            uint32_t v = voff ^ (uint32_t)(((RPI * it >> 2) & 3) * 16);
-            asm volatile("" : "+v"(v));      // formed again each time, not kept in registers
-            dma::dma16(v, srd, 0u, tile + (uint32_t)(PER * wave + it) * 1024u);
-            base += (int64_t)RPI * (ld2 / 2);
+            v[it] = voff ^ (uint32_t)(((RPI * it >> 2) & 3) * 16);
+            asm volatile("" : "+v"(v[it]));      // formed again each time, not kept in registers
+        }
+        if (left >= BLK) {
+            const auto srd = dma::make_srd(base, 16u * ld2);
+            if constexpr (D == 128)
+                asm volatile("s_mov_b32 m0, %8\n\ts_nop 0\n\t"
+                             "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
+                             "buffer_load_dwordx4 %1, %4, %5 offen offset:1024 lds\n\t"
+                             "buffer_load_dwordx4 %2, %4, %6 offen offset:2048 lds\n\t"
+                             "buffer_load_dwordx4 %3, %4, %7 offen offset:3072 lds"
+                             ::"v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(srd), "s"(step), "s"(2 * step), "s"(3 * step), "s"(lds) : "memory", "m0");
+            else
+                asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\t"
+                             "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
+                             "buffer_load_dwordx4 %1, %2, %3 offen offset:1024 lds"
+                             ::"v"(v[0]), "v"(v[1]), "s"(srd), "s"(step), "s"(lds) : "memory", "m0");
+        } else {      // the descriptor ends behind the last row
+            left -= 16 * wave;
+#pragma unroll
+            for (int it = 0; it < PER; ++it) {
+                const int n = min(left - RPI * it, RPI);
+                dma::dma16(v[it], dma::make_srd(base + (uint64_t)(RPI * it) * ld2, n <= 0 ? 0u : (uint32_t)(n - 1) * ld2 + 2u * D), 0u, lds + 1024u * it);
+            }
         }
     }
 };

@@ -64,10 +64,9 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
     const TileLoad<D> load(ld);
     const TileRead<D> rd(lds0);
     auto fetch = [&](int tile, int buf) {
-        const int64_t off = (int64_t)tile * BLK * ld;
-        const int rows = s.len - tile * BLK;
-        load.issue(gk + off, rows, lds0 + (uint32_t)buf * (PAIR<D> * 2u), wave);
-        load.issue(gv + off, rows, lds0 + (uint32_t)buf * (PAIR<D> * 2u) + TILE<D> * 2u, wave);
+        const uint32_t at = lds0 + (uint32_t)buf * (PAIR<D> * 2u);
+        load.issue(gk, tile, s.len - tile * BLK, at, wave);
+        load.issue(gv, tile, s.len - tile * BLK, at + TILE<D> * 2u, wave);
     };
     fetch(tile_at(0), 0);
 
@@ -192,6 +191,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
             floatx16 S[2];
             scores(r0, 0, S[0]);
             scores(r0, 1, S[1]);
+            attn::interleave<4, 1, 1, D / 8 - 4, 4>();
             uint32_t pk[2][8];
             probabilities(S, pk);
             // o^T[column][query] += v^T[column][key] p^T[key][query], 16 keys at a time
@@ -201,6 +201,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
 #pragma unroll
                 for (int i = 0; i < NC; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.columns(TILE<D>, i, ks), fp, O[i], 0, 0, 0);
             }
+            attn::interleave<8, 1, 2, 4 * NC - 4, 4>();
         }
     }
 
