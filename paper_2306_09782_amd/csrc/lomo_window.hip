@@ -12,8 +12,8 @@
 // and rounds.  All recompute S, P, dP, dS in blocks of 32 x 32 per wave with the wave's own rows along the lanes.
 //
 // fp32 accumulation on the matrix cores.  P and dS pass through fp16 before the products that consume them; P is held times 2^15 there,
-// so that the probabilities of a long window (2^-14 and less) keep all their bits.  dq, dk, dv are rounded once.  Blocks that a mask
-// cuts look for inf and NaN and take them out of the products, so that a pair which the mask hides adds nothing.
+// so that the probabilities of a long window (2^-14 and less) keep all their bits.  dq, dk, dv are rounded once.  Tiles that a mask cuts are
+// made finite first, so that a pair which the mask hides adds nothing.
 #include "lomo_window_common.h"
 
 #include <algorithm>
@@ -80,13 +80,6 @@ __device__ __forceinline__ void products(const TileRead<D>& r0, const half8 (&fx
     __builtin_amdgcn_sched_barrier(0);
 }
 
-__device__ __forceinline__ bool any_not_finite(const floatx16& S, const floatx16& P) {
-    bool bad = false;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) bad |= not_finite(S[e]) | not_finite(P[e]);
-    return __any(bad);
-}
-
 // acc[i] += tile^T[column][row] f[row][lane's row], 32 rows at `off` of the tile.
 template <int D>
 __device__ __forceinline__ void multiply(const TileRead<D>& r0, int off, const half8 (&f)[2], floatx16 (&acc)[D / 32]) {
@@ -97,23 +90,6 @@ __device__ __forceinline__ void multiply(const TileRead<D>& r0, int off, const h
     attn::interleave<4, 1, 2, D / 16 - 2, 2>();
     __builtin_amdgcn_sched_barrier(0);
 }
-// The same; dirty: without what is not finite in the tile.
-template <int D>
-__device__ __forceinline__ void multiply_finite(const TileRead<D>& r0, int off, const half8 (&f)[2], floatx16 (&acc)[D / 32], bool dirty) {
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-        half8 x[D / 32];
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) x[i] = r0.columns(off, i, ks);
-        if (dirty) {
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) x[i] = finite_or_zero(x[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i], f[ks], acc[i], 0, 0, 0);
-    }
-}
-
 template <int N>
 __device__ __forceinline__ void clear(floatx16 (&x)[N]) {
 #pragma unroll
@@ -184,7 +160,7 @@ struct QueryTiles {
     int wave, lane;
     float stat = 0.f;
     __device__ __forceinline__ QueryTiles(const BwdArgs& a, const Rows& s, uint32_t lds0, float* stats)
-        : a(a), s(s), load_q((int64_t)(a.b.h + 2 * a.b.g) * D), load_do((int64_t)a.b.h * D),
+        : a(a), s(s), load_q((int64_t)(a.b.h + 2 * a.b.g) * D, threadIdx.x >> 6), load_do((int64_t)a.b.h * D, threadIdx.x >> 6),
           q(a.qkv + (int64_t)s.start * ((a.b.h + 2 * a.b.g) * D)), dO(a.dO + (int64_t)s.start * (a.b.h * D)), lds0(lds0), stats(stats),
           wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63) {
         stat0 = (wave == 0 ? a.lse : a.delta) + (int64_t)s.start * a.b.h;
@@ -242,7 +218,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
     const int extra = sinks > 0 && first > 0 ? 1 : 0, tiles = last - first + 1 + extra;
     auto tile_at = [&](int i) { return i < extra ? 0 : first + i - extra; };
 
-    const TileLoad<D> load(ld);
+    const TileLoad<D> load(ld, wave);
     const TileRead<D> rd(lds0);
     auto fetch = [&](int tile, int buf) {
         const uint32_t at = lds0 + (uint32_t)buf * (PAIR<D> * 2u);
@@ -266,10 +242,9 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
     clear(acc);
 
     // dS of keys k0 .. k0 + 31 as fragments
-    auto gradients = [&](const TileRead<D>& r0, int k0, auto cut, half8 (&f)[2], bool& dirty) {
+    auto gradients = [&](const TileRead<D>& r0, int k0, auto cut, half8 (&f)[2]) {
         floatx16 S, P;
         products<D>(r0, fq, fd, S, P);
-        dirty = decltype(cut)::value && any_not_finite(S, P);
         uint32_t pk[8];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -304,15 +279,16 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
         for (; it < tiles && !(it >= extra && tile_at(it) >= whole0 && tile_at(it) <= whole1); ++it) {
             const int k0 = tile_at(it) * BLK;
             const TileRead<D> r0 = begin();
+            make_finite<D>(lds0 + (uint32_t)(it & 1) * (PAIR<D> * 2u), wave);
+            attn::meet();
             if (!active) continue;
 #pragma nounroll
             for (int h = 0; h < 2; ++h) {
                 if (seen(qw, k0 + 32 * h, window, sinks) == NONE) continue;
                 const TileRead<D> r1 = r0.at(32 * h * D);
                 half8 f[2];
-                bool dirty;
-                gradients(r1, k0 + 32 * h, std::true_type{}, f, dirty);
-                multiply_finite<D>(r1, 0, f, acc, dirty);
+                gradients(r1, k0 + 32 * h, std::true_type{}, f);
+                multiply<D>(r1, 0, f, acc);
             }
         }
         for (; it < tiles && tile_at(it) <= whole1; ++it) {
@@ -322,8 +298,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
             for (int h = 0; h < 2; ++h) {
                 const TileRead<D> r1 = r0.at(32 * h * D);
                 half8 f[2];
-                bool dirty;
-                gradients(r1, 0, std::false_type{}, f, dirty);
+                gradients(r1, 0, std::false_type{}, f);
                 multiply<D>(r1, 0, f, acc);
             }
         }
@@ -431,6 +406,9 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
             const int qb = tile * BLK, buf = begin();
             // distances in each half: between qb + 32 h - (kw + 31) and qb + 32 h + 31 - kw
             auto some = [&](int h) { return active && qb + 32 * h + 31 - kw >= near && (near > 0 || qb + 32 * h - (kw + 31) < (int)reach); };
+            make_finite<D>(lds0 + (uint32_t)buf * (PAIR<D> * 2u), wave);
+            make_finite<D>(lds0 + (uint32_t)buf * (PAIR<D> * 2u) + TILE<D> * 2u, wave);
+            attn::meet();
             half8 f[2], g[2];
             if (some(part)) own_gradients(buf, qb + 32 * part + 4 * lh - key - near, std::true_type{}, f);
             attn::meet();
@@ -441,7 +419,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
                 xch.get(g);
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks) g[ks] = h == part ? f[ks] : g[ks];
-                multiply_finite<D>(r0, 0, g, acc, any_not_finite<D>(r0, 0));
+                multiply<D>(r0, 0, g, acc);
             }
         }
         while (it < steps && whole()) {

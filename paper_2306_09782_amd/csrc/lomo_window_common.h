@@ -90,45 +90,47 @@ __device__ __forceinline__ int swz(int r) {
     else return ((r & 2) << 1) | ((r >> 2) & 3);
 }
 
-// Load of [64 x D] tiles of rows `ld` elements apart, 64 of them less than 4 GiB.  A wave fetches 16 neighbouring rows, RPI with an
+// Load of [TROWS x D] tiles of rows `ld` elements apart, 64 of them less than 4 GiB.  A wave fetches WROWS neighbouring rows, RPI with an
 // instruction.  The instructions' swizzles differ from that of the first in two chunk bits; their offsets in memory and in LDS share the
 // immediate, so that one value of M0 serves them all.
-template <int D>
+template <int D, int TROWS = BLK>
 struct TileLoad {
-    static constexpr int RPI = 512 / D, PER = 16 / RPI;
+    static constexpr int WROWS = TROWS / 4, RPI = 512 / D, PER = WROWS / RPI;
     uint32_t voff, ld2, step;
-    __device__ __forceinline__ TileLoad(int64_t ld) {
+    __device__ __forceinline__ TileLoad(int64_t ld, int wave) {
         const int lane = threadIdx.x & 63, rr = lane / (D / 8), c = lane % (D / 8);
         ld2 = 2u * (uint32_t)ld;
         step = RPI * ld2 - 1024u;      // what the scalar offset adds to the immediate
-        voff = (uint32_t)rr * ld2 + (uint32_t)((c ^ swz<D>(rr)) * 16);
+        voff = (uint32_t)rr * ld2 + (uint32_t)((c ^ swz<D>(rr) ^ ((WROWS * wave >> 2) & 3)) * 16);
     }
     // Row 0 of the tile is `tile` tiles from `rows0`, `left` rows of the sequence remain from there (any number); the others become zeros.
     __device__ __forceinline__ void issue(const uint16_t* rows0, int tile, int left, uint32_t lds, int wave) const {
-        const char* base = reinterpret_cast<const char*>(rows0) + (uint64_t)(uint32_t)tile * (64u * ld2) + (uint64_t)((uint32_t)wave * 16u * ld2);
-        lds += (uint32_t)wave * (16u * D * 2u);
+        const char* base = reinterpret_cast<const char*>(rows0) + (uint64_t)(uint32_t)tile * (TROWS * ld2) + (uint64_t)((uint32_t)wave * WROWS * ld2);
+        lds += (uint32_t)wave * (WROWS * D * 2u);
         uint32_t v[PER];
 #pragma unroll
         for (int it = 0; it < PER; ++it) {
             v[it] = voff ^ (uint32_t)(((RPI * it >> 2) & 3) * 16);
             asm volatile("" : "+v"(v[it]));      // formed again each time, not kept in registers
         }
-        if (left >= BLK) {
-            const auto srd = dma::make_srd(base, 16u * ld2);
-            if constexpr (D == 128)
+        if (left >= TROWS) {
+            const auto srd = dma::make_srd(base, WROWS * ld2);
+            if constexpr (PER == 4)
                 asm volatile("s_mov_b32 m0, %8\n\ts_nop 0\n\t"
                              "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
                              "buffer_load_dwordx4 %1, %4, %5 offen offset:1024 lds\n\t"
                              "buffer_load_dwordx4 %2, %4, %6 offen offset:2048 lds\n\t"
                              "buffer_load_dwordx4 %3, %4, %7 offen offset:3072 lds"
                              ::"v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(srd), "s"(step), "s"(2 * step), "s"(3 * step), "s"(lds) : "memory", "m0");
+            else if constexpr (PER == 1)
+                asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(v[0]), "s"(srd), "s"(lds) : "memory", "m0");
             else
                 asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\t"
                              "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
                              "buffer_load_dwordx4 %1, %2, %3 offen offset:1024 lds"
                              ::"v"(v[0]), "v"(v[1]), "s"(srd), "s"(step), "s"(lds) : "memory", "m0");
         } else {      // the descriptor ends behind the last row
-            left -= 16 * wave;
+            left -= WROWS * wave;
 #pragma unroll
             for (int it = 0; it < PER; ++it) {
                 const int n = min(left - RPI * it, RPI);
@@ -195,40 +197,34 @@ __device__ __forceinline__ void store_rows(const floatx16 (&acc)[N], uint16_t* r
     }
 }
 
-// Whether any of a block's 32 rows [32 x D] in a tile holds inf or NaN.
-template <int D>
-__device__ __forceinline__ bool any_not_finite(const TileRead<D>& r0, int off) {
-    uint32_t worst = 0;
+// A product over a block that a mask cuts has zeros for the hidden pairs, and 0 * inf is not 0: the moving operand of such tiles is made
+// finite in LDS first.  What sees the values all the same gets to know of them otherwise: their rows' lse and delta are not finite,
+// and the forward adds them.  Each wave looks through the rows that it fetched; returned is one bit for each row that held any (uniform).
+template <int D, int TROWS = BLK>
+__device__ __forceinline__ uint32_t make_finite(uint32_t tile, int wave) {
+    typedef __attribute__((address_space(3))) u32x4* chunk_p;
+    using Load = TileLoad<D, TROWS>;
+    constexpr int RPI = Load::RPI, LANES = 64 / RPI;      // of a row
+    const int lane = threadIdx.x & 63;
+    uint32_t rows = 0;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-        const u32x4 w = __builtin_bit_cast(u32x4, r0.rows(off, ks));
+    for (int it = 0; it < Load::PER; ++it) {
+        chunk_p at = (chunk_p)(tile + (uint32_t)wave * (Load::WROWS * D * 2u) + (uint32_t)it * 1024u + (uint32_t)lane * 16u);
+        u32x4 w = *at;
+        uint32_t any = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) worst |= ((w[e] & 0x7c007c00u) + 0x04000400u) & 0x80008000u;      // an exponent of ones carries over
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t bad = (((w[e] & 0x7c007c00u) + 0x04000400u) & 0x80008000u) >> 15;      // an exponent of ones carries over
+            any |= bad;
+            w[e] &= ~(bad * 0xffffu);
+        }
+        const uint64_t lanes = __ballot(any != 0);
+        if (lanes == 0) continue;
+        *at = w;
+#pragma unroll
+        for (int r = 0; r < RPI; ++r) rows |= ((lanes >> (r * LANES)) & ((1ull << LANES) - 1)) != 0 ? 1u << (RPI * it + r) : 0u;
     }
-    return __any(worst != 0);
-}
-__device__ __forceinline__ half8 finite_or_zero(half8 x) {
-    u32x4 w = __builtin_bit_cast(u32x4, x);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const uint32_t bad = (((w[e] & 0x7c007c00u) + 0x04000400u) & 0x80008000u) >> 15;      // 1 in each half that is not finite
-        w[e] &= ~(bad * 0xffffu);
-    }
-    return __builtin_bit_cast(half8, w);
-}
-// 1 for inf, 64 for -inf, 4096 for NaN, 0 for the rest; up to 32 of these added are told apart again.
-__device__ __forceinline__ half8 not_finite_code(half8 x) {
-    half8 c;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float f = (float)x[e];
-        c[e] = f == INFINITY ? (_Float16)1.f : f == -INFINITY ? (_Float16)64.f : f != f ? (_Float16)4096.f : (_Float16)0.f;
-    }
-    return c;
-}
-__device__ __forceinline__ float sum_of_codes(float sum) {
-    const uint32_t n = (uint32_t)sum, up = n & 63u, down = (n >> 6) & 63u;
-    return n >= 4096u || (up && down) ? NAN : up ? INFINITY : down ? -INFINITY : 0.f;
+    return rows;
 }
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 

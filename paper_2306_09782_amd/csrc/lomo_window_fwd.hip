@@ -8,8 +8,8 @@
 // rounded to fp16 relative to the running maximum, as the matrix cores take them; sums and accumulators are fp32; o is rounded once.
 // Deterministic, and independent of what else is in the batch.
 //
-// A key that the mask hides from a query adds nothing to it, whatever its v holds: blocks that a mask cuts look for inf and NaN and
-// take those out of the product, adding them to the queries that do see them.
+// A key that the mask hides from a query adds nothing to it, whatever its v holds: inf and NaN are taken out of the tiles that a mask
+// cuts, and added to the queries that do see them.
 #include "lomo_window_common.h"
 
 namespace lomo {
@@ -26,10 +26,12 @@ struct FwdArgs {
 
 }  // namespace win
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::FwdArgs a) {
+template <int D, int KEYS, int WAVES>
+__global__ __launch_bounds__(256, WAVES) void window_attention_forward_kernel(win::FwdArgs a) {
     using namespace win;
-    extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // two pairs of tiles: K, V
+    extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // two pairs of tiles of KEYS rows: K, V
+    __shared__ uint32_t bad[2][4];                                        // rows of a V tile that are not finite, by wave
+    constexpr int HALVES = KEYS / 32, KTILE = KEYS * D, KPAIR = 2 * KTILE;
     constexpr float C2 = SCALE<D> * LOG2E;
 
     const int lane = threadIdx.x & 63;
@@ -56,17 +58,17 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
     const uint16_t* gk = a.qkv + (int64_t)s.start * ld + (int64_t)(a.b.h + kv) * D;
     const uint16_t* gv = gk + (int64_t)a.b.g * D;
 
-    // tiles of this workgroup: the sinks' where it is not among those of the window
-    const int first = max(0, q0 - window + 1) / BLK, last = min(q0 + ROWS - 1, s.len - 1) / BLK;
-    const int extra = sinks > 0 && first > 0 ? 1 : 0, tiles = last - first + 1 + extra;
-    auto tile_at = [&](int i) { return i < extra ? 0 : first + i - extra; };
+    // tiles of this workgroup: the sinks' where they are not among those of the window
+    const int first = max(0, q0 - window + 1) / KEYS, last = min(q0 + ROWS - 1, s.len - 1) / KEYS;
+    const int extra = min((sinks + KEYS - 1) / KEYS, first), tiles = last - first + 1 + extra;
+    auto tile_at = [&](int i) { return i < extra ? i : first + i - extra; };
 
-    const TileLoad<D> load(ld);
+    const TileLoad<D, KEYS> load(ld, wave);
     const TileRead<D> rd(lds0);
     auto fetch = [&](int tile, int buf) {
-        const uint32_t at = lds0 + (uint32_t)buf * (PAIR<D> * 2u);
-        load.issue(gk, tile, s.len - tile * BLK, at, wave);
-        load.issue(gv, tile, s.len - tile * BLK, at + TILE<D> * 2u, wave);
+        const uint32_t at = lds0 + (uint32_t)buf * (KPAIR * 2u);
+        load.issue(gk, tile, s.len - tile * KEYS, at, wave);
+        load.issue(gv, tile, s.len - tile * KEYS, at + KTILE * 2u, wave);
     };
     fetch(tile_at(0), 0);
 
@@ -92,10 +94,10 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
     // From scores to probabilities relative to the running maximum, in fp16.  The maximum moves only where it has grown by more than
     // SLACK: probabilities stay below 2^SLACK, and most tiles leave sum and output as they are.
     constexpr float SLACK = 8.f;
-    auto probabilities = [&](floatx16 (&S)[2], uint32_t (&pk)[2][8]) {
+    auto probabilities = [&](const floatx16 (&S)[HALVES], uint32_t (&pk)[HALVES][8]) {
         float top = -INFINITY;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < HALVES; ++h)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, S[h][e]);
         const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
@@ -112,7 +114,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
         const float m_ref = m_run == -INFINITY ? 0.f : m_run;      // a query that has seen no key yet
         float sum = 0.f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < HALVES; ++h)
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(fmaf(S[h][e], C2, -m_ref)), p1 = __builtin_amdgcn_exp2f(fmaf(S[h][e + 1], C2, -m_ref));
@@ -127,81 +129,77 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
         // the tiles have landed; everybody is done with the other pair
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (it + 1 < tiles) fetch(tile_at(it + 1), (it + 1) & 1);      // in flight while this pair is multiplied
-        return rd.at((it & 1) * PAIR<D>);
+        return rd.at((it & 1) * KPAIR);
+    };
+    // o^T[column][query] += v^T[column][key] p^T[key][query], 16 keys at a time
+    auto values = [&](const TileRead<D>& r0, const uint32_t (&pk)[HALVES][8]) {
+#pragma unroll
+        for (int ks = 0; ks < 2 * HALVES; ++ks) {
+            const half8 fp = fragment_of(pk[ks >> 1], ks & 1);
+#pragma unroll
+            for (int i = 0; i < NC; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.columns(KTILE, i, ks), fp, O[i], 0, 0, 0);
+        }
+        attn::interleave<8, 1, 2, 2 * HALVES * NC - 4, 4>();
+    };
+    auto all_scores = [&](const TileRead<D>& r0, floatx16 (&S)[HALVES]) {
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) scores(r0, h, S[h]);
+        attn::interleave<4, 1, 1, HALVES * D / 16 - 4, 4>();
     };
     // the tiles that every query of the workgroup sees whole
-    const int whole0 = (max(0, q0 + ROWS - window) + BLK - 1) / BLK, whole1 = q0 / BLK - 1;
+    const int whole0 = (max(0, q0 + ROWS - window) + KEYS - 1) / KEYS, whole1 = q0 / KEYS - 1;
     while (it < tiles) {
         for (; it < tiles && !(it >= extra && tile_at(it) >= whole0 && tile_at(it) <= whole1); ++it) {
-            const int k0 = tile_at(it) * BLK;
+            const int k0 = tile_at(it) * KEYS;
             const TileRead<D> r0 = begin();
+            const uint32_t mine = make_finite<D, KEYS>(lds0 + (uint32_t)(it & 1) * (KPAIR * 2u) + KTILE * 2u, wave);
+            if (lane == 0) bad[it & 1][wave] = mine;
+            attn::meet();
             if (!active) continue;
-            const Seen seen_of[2] = {seen(qw, k0, window, sinks), seen(qw, k0 + 32, window, sinks)};
-            if (seen_of[0] == NONE && seen_of[1] == NONE) continue;
-            auto hidden = [&](int key) { return key > query | (query - key >= window & key >= sinks); };
-            floatx16 S[2];
+            bool none = true;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (seen_of[h] != NONE) scores(r0, h, S[h]);
+            for (int h = 0; h < HALVES; ++h) none = none && seen(qw, k0 + 32 * h, window, sinks) == NONE;
+            if (none) continue;
+            // of a distance that is negative or not below the window, but for the sinks
+            auto hidden = [&](int key) { return (uint32_t)(query - key) >= (key < sinks ? 0x80000000u : (uint32_t)window); };
+            floatx16 S[HALVES];
+            all_scores(r0, S);
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const bool no = seen_of[h] == NONE | hidden(k0 + 32 * h + 8 * (e >> 2) + 4 * lh + (e & 3));
-                    S[h][e] = no ? -INFINITY : S[h][e];
+                    S[h][e] = hidden(k0 + 32 * h + 8 * (e >> 2) + 4 * lh + (e & 3)) ? -INFINITY : S[h][e];
+                    if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
-            }
-            uint32_t pk[2][8];
+            uint32_t pk[HALVES][8];
             probabilities(S, pk);
-#pragma nounroll
-            for (int h = 0; h < 2; ++h) {
-                if (seen_of[h] == NONE) continue;
-                const TileRead<D> r1 = r0.at(32 * h * D);
-                const bool dirty = any_not_finite<D>(r1, TILE<D>);
-                uint32_t own[8], see[8];
+            values(r0, pk);
+            uint64_t rows = 0;
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const int key = k0 + 32 * h + 8 * (e >> 2) + 4 * lh + (e & 3);
-                    own[e >> 1] = h == 0 ? pk[0][e >> 1] : pk[1][e >> 1];
-                    see[e >> 1] = (hidden(key) ? 0u : 0x3c00u) | (hidden(key + 1) ? 0u : 0x3c000000u);
-                }
-                const half8 fp[2] = {fragment_of(own, 0), fragment_of(own, 1)};
+            for (int w = 0; w < 4; ++w) rows |= (uint64_t)bad[it & 1][w] << (KEYS / 4 * w);
+            while (rows != 0) {      // what is not finite, to the queries that see its key
+                const int key = k0 + __builtin_ctzll(rows);
+                rows &= rows - 1;
+                if (hidden(key)) continue;
+                const uint16_t* v = gv + (int64_t)key * ld + 4 * lh;
 #pragma unroll
-                for (int i = 0; i < NC; ++i) {
-                    half8 v[2] = {r1.columns(TILE<D>, i, 0), r1.columns(TILE<D>, i, 1)};
-                    floatx16 n;
+                for (int i = 0; i < NC; ++i)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) n[e] = 0.f;
-                    if (dirty) {      // what is not finite is left out, and added to the queries that see its key
-                        const half8 fs[2] = {fragment_of(see, 0), fragment_of(see, 1)};
+                    for (int g4 = 0; g4 < 4; ++g4) {
+                        const half4 x = *reinterpret_cast<const half4*>(v + 32 * i + 8 * g4);
 #pragma unroll
-                        for (int ks = 0; ks < 2; ++ks) {
-                            n = __builtin_amdgcn_mfma_f32_32x32x16_f16(not_finite_code(v[ks]), fs[ks], n, 0, 0, 0);
-                            v[ks] = finite_or_zero(v[ks]);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) O[i][e] += sum_of_codes(n[e]);
+                        for (int e = 0; e < 4; ++e) O[i][4 * g4 + e] += not_finite((float)x[e]) ? (float)x[e] : 0.f;
                     }
-#pragma unroll
-                    for (int ks = 0; ks < 2; ++ks) O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[ks], fp[ks], O[i], 0, 0, 0);
-                }
             }
         }
         for (; it < tiles && tile_at(it) <= whole1; ++it) {
             const TileRead<D> r0 = begin();
             if (!active) continue;
-            floatx16 S[2];
-            scores(r0, 0, S[0]);
-            scores(r0, 1, S[1]);
-            attn::interleave<4, 1, 1, D / 8 - 4, 4>();
-            uint32_t pk[2][8];
+            floatx16 S[HALVES];
+            all_scores(r0, S);
+            uint32_t pk[HALVES][8];
             probabilities(S, pk);
-            // o^T[column][query] += v^T[column][key] p^T[key][query], 16 keys at a time
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                const half8 fp = fragment_of(pk[ks >> 1], ks & 1);
-#pragma unroll
-                for (int i = 0; i < NC; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.columns(TILE<D>, i, ks), fp, O[i], 0, 0, 0);
-            }
-            attn::interleave<8, 1, 2, 4 * NC - 4, 4>();
+            values(r0, pk);
         }
     }
 
@@ -219,10 +217,10 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
     if (own && lh == 0) a.lse[t * a.b.h + n] = (m_run + __builtin_amdgcn_logf(l)) * LN2;
 }
 
-template <int D>
+template <int D, int KEYS, int WAVES>
 static hipError_t launch_forward_of(const win::FwdArgs& a, hipStream_t st) {
-    auto kern = window_attention_forward_kernel<D>;
-    constexpr int lds = 2 * win::PAIR<D> * 2;
+    auto kern = window_attention_forward_kernel<D, KEYS, WAVES>;
+    constexpr int lds = 2 * 2 * KEYS * D * 2;
     static const hipError_t cfg = allow_dynamic_lds(kern, lds);
     if (cfg != hipSuccess) return cfg;
     hipLaunchKernelGGL(kern, dim3((unsigned)a.total), dim3(256), lds, st, a);
@@ -236,7 +234,7 @@ hipError_t launch_window_attention_forward(const uint16_t* qkv, uint16_t* o, flo
     a.qkv = qkv; a.o = o; a.lse = lse;
     a.numbers = (int)win::pieces(T, B, win::ROWS, 1);
     a.total = (int)(a.numbers * h);
-    return d == 128 ? launch_forward_of<128>(a, st) : launch_forward_of<64>(a, st);
+    return d == 128 ? launch_forward_of<128, 64, 2>(a, st) : launch_forward_of<64, 64, 2>(a, st);
 }
 
 }  // namespace lomo
