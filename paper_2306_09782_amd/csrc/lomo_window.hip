@@ -25,6 +25,10 @@ namespace win {
 
 constexpr int FAR_ROWS = 512;
 constexpr float P_SCALE = 32768.f, P_LOG2 = 15.f;
+template <int D>
+constexpr float DS_SCALE = SCALE<D> / P_SCALE;      // of dP - delta where it meets P times P_SCALE
+template <int D>
+constexpr float SCALE_LOG2 = D == 128 ? 3.5f : 3.f;      // log2(sqrt(D))
 
 struct BwdArgs {
     Batch b;
@@ -99,7 +103,7 @@ __device__ __forceinline__ void clear(floatx16 (&x)[N]) {
 }
 
 // P (times P_SCALE) and dS of a block as fragments, for a wave that owns keys: queries qb .. qb + 31 (rows 0 .. 31 of the pair q, do;
-// stats: their lse log2(e) - 15 and, BLK further on, delta) against the lane's key.  CUT: without the pairs whose distance is not one of the
+// stats: their lse log2(e) - 15 and, BLK further on, delta DS_SCALE) against the lane's key.  CUT: without the pairs whose distance is not one of the
 // `reach` from `near` on.
 template <int D, bool CUT>
 __device__ __forceinline__ void key_gradients(const TileRead<D>& r0, const float* stats, const half8 (&fk)[D / 16], const half8 (&fv)[D / 16],
@@ -114,7 +118,7 @@ __device__ __forceinline__ void key_gradients(const TileRead<D>& r0, const float
         const float lq[4] = {l4.x, l4.y, l4.z, l4.w}, dq[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            float p = __builtin_amdgcn_exp2f(fmaf(C2, S[4 * g4 + e], -lq[e])), d = P[4 * g4 + e] - dq[e];
+            float p = __builtin_amdgcn_exp2f(fmaf(C2, S[4 * g4 + e], -lq[e])), d = fmaf(DS_SCALE<D>, P[4 * g4 + e], -dq[e]);
             if constexpr (CUT) {
                 p = not_finite(d) ? NAN : p;
                 asm volatile("" : "+v"(p), "+v"(d));      // selects, no branches
@@ -130,7 +134,7 @@ __device__ __forceinline__ void key_gradients(const TileRead<D>& r0, const float
 #pragma unroll
     for (int e = 0; e < 16; e += 2) {
         pp[e >> 1] = pack2(S[e], S[e + 1]);
-        pd[e >> 1] = pack2(SCALE<D> / P_SCALE * S[e] * P[e], SCALE<D> / P_SCALE * S[e + 1] * P[e + 1]);
+        pd[e >> 1] = pack2(S[e] * P[e], S[e + 1] * P[e + 1]);
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -178,7 +182,7 @@ struct QueryTiles {
     }
     // this wave's share of what fetch() brought; a barrier has to follow
     __device__ __forceinline__ void keep_stats(int buf) const {
-        if (wave < 2) stats[(2 * buf + wave) * BLK + lane] = wave == 0 ? fmaf(stat, LOG2E, -P_LOG2) : stat;
+        if (wave < 2) stats[(2 * buf + wave) * BLK + lane] = wave == 0 ? fmaf(stat, LOG2E, -P_LOG2) : stat * DS_SCALE<D>;
     }
 };
 
@@ -234,7 +238,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
         load_fragments<D>(fd, a.dO + t * ldo + (int64_t)n * D);
         half8 fo[D / 16];
         load_fragments<D>(fo, a.o + t * ldo + (int64_t)n * D);
-        lq = a.lse[t * a.b.h + n] * LOG2E;
+        lq = fmaf(a.lse[t * a.b.h + n], LOG2E, SCALE_LOG2<D>);      // so that P comes with the scale of dS
         delta = row_product<D>(fo, fd);
         if (lh == 0 && query < s.len) a.delta[t * a.b.h + n] = delta;
     }
@@ -248,7 +252,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
         uint32_t pk[8];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            S[e] = SCALE<D> * __builtin_amdgcn_exp2f(fmaf(C2, S[e], -lq));
+            S[e] = __builtin_amdgcn_exp2f(fmaf(C2, S[e], -lq));
             P[e] -= delta;
             if constexpr (decltype(cut)::value) {
                 const int key = k0 + 8 * (e >> 2) + 4 * lh + (e & 3);
@@ -318,7 +322,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int part = wave >> 1, l32 = lane & 31, lh = lane >> 5;
-    float* stats = reinterpret_cast<float*>(smem);      // [pair][lse log2(e) - 15 | delta][64]
+    float* stats = reinterpret_cast<float*>(smem);      // [pair][lse log2(e) - 15 | delta DS_SCALE][64]
     uint16_t* tiles_at = smem + STAT_BYTES / 2;
     const uint32_t lds0 = (uint32_t)(uintptr_t)tiles_at;
     const attn::Exchange xch(tiles_at + 2 * PAIR<D>, wave);
@@ -398,6 +402,8 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) f[ks] = part == 0 ? fp[ks] : fd[ks];
     };
+    // where half h of do (for dv) or q (for dk) is
+    auto sums_of = [&](int buf, int h) { return rd.at(buf * PAIR<D> + (part == 0 ? TILE<D> : 0) + 32 * h * D); };
     // the query tiles that are within the bounds for every key of the workgroup
     const int whole0 = (k0 + BLK - 1 + near + BLK - 1) / BLK, whole1 = near > 0 ? last : (k0 + a.b.window - BLK) / BLK;
     auto whole = [&]() { return tile >= whole0 && tile <= whole1; };
@@ -409,34 +415,28 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
             make_finite<D>(lds0 + (uint32_t)buf * (PAIR<D> * 2u), wave);
             make_finite<D>(lds0 + (uint32_t)buf * (PAIR<D> * 2u) + TILE<D> * 2u, wave);
             attn::meet();
-            half8 f[2], g[2];
-            if (some(part)) own_gradients(buf, qb + 32 * part + 4 * lh - key - near, std::true_type{}, f);
+            half8 f[2];
+            if (some(part)) {
+                own_gradients(buf, qb + 32 * part + 4 * lh - key - near, std::true_type{}, f);
+                multiply<D>(sums_of(buf, part), 0, f, acc);
+            }
             attn::meet();
-#pragma nounroll
-            for (int h = 0; h < 2; ++h) {
-                if (!some(h)) continue;
-                const TileRead<D> r0 = rd.at(buf * PAIR<D> + (part == 0 ? TILE<D> : 0) + 32 * h * D);
-                xch.get(g);
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) g[ks] = h == part ? f[ks] : g[ks];
-                multiply<D>(r0, 0, g, acc);
+            if (some(1 - part)) {
+                xch.get(f);
+                multiply<D>(sums_of(buf, 1 - part), 0, f, acc);
             }
         }
         while (it < steps && whole()) {
             const int buf = begin();
-            half8 f[2], g[2];
-            if (active) own_gradients(buf, 0, std::false_type{}, f);
+            half8 f[2];
+            if (active) {
+                own_gradients(buf, 0, std::false_type{}, f);
+                multiply<D>(sums_of(buf, part), 0, f, acc);
+            }
             attn::meet();
             if (!active) continue;
-            const TileRead<D> r0 = rd.at(buf * PAIR<D> + (part == 0 ? TILE<D> : 0));
-            xch.get(g);
-            if (part == 0) {
-                multiply<D>(r0, 0, f, acc);
-                multiply<D>(r0, 32 * D, g, acc);
-            } else {
-                multiply<D>(r0, 0, g, acc);
-                multiply<D>(r0, 32 * D, f, acc);
-            }
+            xch.get(f);
+            multiply<D>(sums_of(buf, 1 - part), 0, f, acc);
         }
     }
     if (!active) return;
