@@ -163,10 +163,10 @@ struct QueryTiles {
     float* stats;
     int wave, lane;
     float stat = 0.f;
-    __device__ __forceinline__ QueryTiles(const BwdArgs& a, const Rows& s, uint32_t lds0, float* stats)
-        : a(a), s(s), load_q((int64_t)(a.b.h + 2 * a.b.g) * D, threadIdx.x >> 6), load_do((int64_t)a.b.h * D, threadIdx.x >> 6),
+    __device__ __forceinline__ QueryTiles(const BwdArgs& a, const Rows& s, uint32_t lds0, float* stats, int wave)
+        : a(a), s(s), load_q((int64_t)(a.b.h + 2 * a.b.g) * D, wave), load_do((int64_t)a.b.h * D, wave),
           q(a.qkv + (int64_t)s.start * ((a.b.h + 2 * a.b.g) * D)), dO(a.dO + (int64_t)s.start * (a.b.h * D)), lds0(lds0), stats(stats),
-          wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63) {
+          wave(wave), lane(threadIdx.x & 63) {
         stat0 = (wave == 0 ? a.lse : a.delta) + (int64_t)s.start * a.b.h;
     }
     __device__ __forceinline__ void fetch(int tile, int n, int buf) {
@@ -242,6 +242,9 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
         delta = row_product<D>(fo, fd);
         if (lh == 0 && query < s.len) a.delta[t * a.b.h + n] = delta;
     }
+    arrived<D>(fq);
+    arrived<D>(fd);
+    asm volatile("" : "+v"(lq));
     floatx16 acc[D / 32];
     clear(acc);
 
@@ -311,19 +314,21 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
 }
 
 // A workgroup has 64 keys and the queries whose distance to a key is within some bounds: of the first a.far workgroups the sinks and FAR_ROWS
-// queries beyond the window, of the others a block of keys and the queries whose window reaches it.  Two waves have the same 32 keys; each forms
-// P and dS of one half of the tile's queries, hands one of the two to the other through LDS, and sums dv (the first) or dk over all of them:
-// twice the workgroups of one that has both sums, of which a group of heads leaves few, and half the accumulators.
+// queries beyond the window, of the others a block of keys and the queries whose window reaches it.  Two teams of four waves, with tiles of
+// their own, take one half each of the walk through the tiles of all heads of the group, and the first adds up: a walk is long where heads share
+// their keys, and the longest one bounds a call.  In a team two waves have the same 32 keys; each forms P and dS of one half of the tile's
+// queries, hands one of the two to the other through LDS, and sums dv (the first) or dk over all of them.
 template <int D>
-__global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdArgs a) {
+__global__ __launch_bounds__(512, 2) void window_attention_dkdv_kernel(win::BwdArgs a) {
     using namespace win;
-    extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // lse and delta of two pairs of tiles; the pairs: Q, dO; what waves exchange
+    extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // of each team: lse and delta of two pairs of tiles; the pairs: Q, dO; what waves exchange
 
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
     const int part = wave >> 1, l32 = lane & 31, lh = lane >> 5;
-    float* stats = reinterpret_cast<float*>(smem);      // [pair][lse log2(e) - 15 | delta DS_SCALE][64]
-    uint16_t* tiles_at = smem + STAT_BYTES / 2;
+    uint16_t* own_lds = smem + team * (KEY_LDS_BYTES<D> / 2);
+    float* stats = reinterpret_cast<float*>(own_lds);      // [pair][lse log2(e) - 15 | delta DS_SCALE][64]
+    uint16_t* tiles_at = own_lds + STAT_BYTES / 2;
     const uint32_t lds0 = (uint32_t)(uintptr_t)tiles_at;
     const attn::Exchange xch(tiles_at + 2 * PAIR<D>, wave);
 
@@ -367,23 +372,28 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
     const int64_t ld = (int64_t)(a.b.h + 2 * a.b.g) * D;
     const int64_t t = (int64_t)s.start + min(key, s.len - 1);
 
-    const int per = last - first + 1, steps = per * r;
-    QueryTiles<D> tiles(a, s, lds0, stats);
-    tiles.fetch(first, kv * r, 0);
+    // the walk: (head, tile); this team's steps are `steps` from its `tile` and head `n` on, the other's tile is `other`
+    const int per = last - first + 1, total = per * r, more = (total + 1) / 2, fewer = total - more;      // of the first team, of the second
+    const int steps = team == 0 ? more : fewer;
+    int tile = first + (team == 0 ? 0 : more % per), other = first + (team == 0 ? more % per : 0), n = kv * r + (team == 0 ? 0 : more / per);
+    QueryTiles<D> tiles(a, s, lds0, stats, wave);
+    if (steps > 0) tiles.fetch(tile, n, 0);
 
     half8 fk[D / 16], fv[D / 16];
     if (active) {
         load_fragments<D>(fk, a.qkv + t * ld + (int64_t)(a.b.h + kv) * D);
         load_fragments<D>(fv, a.qkv + t * ld + (int64_t)(a.b.h + a.b.g + kv) * D);
     }
+    arrived<D>(fk);
+    arrived<D>(fv);
     floatx16 acc[D / 32];      // dv or dk
     clear(acc);
     const TileRead<D> rd(lds0);
 
-    int it = 0, tile = first, n = kv * r;      // the pair that is next
+    int it = 0;
     auto begin = [&]() {
         const int buf = it & 1;
-        tiles.keep_stats(buf);
+        if (it < steps) tiles.keep_stats(buf);
         // the tiles have landed; everybody is done with the other pair
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         ++it;
@@ -391,6 +401,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
             tile = first;
             ++n;
         }
+        if (++other > last) other = first;
         if (it < steps) tiles.fetch(tile, n, buf ^ 1);      // in flight while this pair is multiplied
         return buf;
     };
@@ -406,15 +417,17 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
     auto sums_of = [&](int buf, int h) { return rd.at(buf * PAIR<D> + (part == 0 ? TILE<D> : 0) + 32 * h * D); };
     // the query tiles that are within the bounds for every key of the workgroup
     const int whole0 = (k0 + BLK - 1 + near + BLK - 1) / BLK, whole1 = near > 0 ? last : (k0 + a.b.window - BLK) / BLK;
-    auto whole = [&]() { return tile >= whole0 && tile <= whole1; };
-    while (it < steps) {
-        while (it < steps && !whole()) {
-            const int qb = tile * BLK, buf = begin();
-            // distances in each half: between qb + 32 h - (kw + 31) and qb + 32 h + 31 - kw
-            auto some = [&](int h) { return active && qb + 32 * h + 31 - kw >= near && (near > 0 || qb + 32 * h - (kw + 31) < (int)reach); };
+    auto whole = [&](int x) { return x >= whole0 && x <= whole1; };
+    while (it < more) {
+        while (it < more && !(it < fewer && whole(tile) && whole(other))) {
+            const int qb = tile * BLK;
+            const bool has = active && it < steps;
+            const int buf = begin();
             make_finite<D>(lds0 + (uint32_t)buf * (PAIR<D> * 2u), wave);
             make_finite<D>(lds0 + (uint32_t)buf * (PAIR<D> * 2u) + TILE<D> * 2u, wave);
             attn::meet();
+            // distances in each half: between qb + 32 h - (kw + 31) and qb + 32 h + 31 - kw
+            auto some = [&](int h) { return has && qb + 32 * h + 31 - kw >= near && (near > 0 || qb + 32 * h - (kw + 31) < (int)reach); };
             half8 f[2];
             if (some(part)) {
                 own_gradients(buf, qb + 32 * part + 4 * lh - key - near, std::true_type{}, f);
@@ -426,7 +439,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
                 multiply<D>(sums_of(buf, 1 - part), 0, f, acc);
             }
         }
-        while (it < steps && whole()) {
+        while (it < fewer && whole(tile) && whole(other)) {
             const int buf = begin();
             half8 f[2];
             if (active) {
@@ -439,7 +452,21 @@ __global__ __launch_bounds__(256, 2) void window_attention_dkdv_kernel(win::BwdA
             multiply<D>(sums_of(buf, 1 - part), 0, f, acc);
         }
     }
-    if (!active) return;
+    // the second team's sums to the first
+    float* sums = reinterpret_cast<float*>(smem) + wave * (D / 2 * 64) + lane;      // as much as two pairs of tiles
+    __syncthreads();
+    if (team == 1) {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sums[(16 * i + e) * 64] = acc[i][e];
+    }
+    __syncthreads();
+    if (team == 1 || !active) return;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] += sums[(16 * i + e) * 64];
     if (part == 0) {
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
@@ -501,10 +528,10 @@ static hipError_t launch_backward_of(const win::BwdArgs& a, hipStream_t st) {
     auto dkdv = window_attention_dkdv_kernel<D>;
     static const hipError_t cfg0 = allow_dynamic_lds(dq, DQ_LDS_BYTES<D>);
     if (cfg0 != hipSuccess) return cfg0;
-    static const hipError_t cfg1 = allow_dynamic_lds(dkdv, KEY_LDS_BYTES<D>);
+    static const hipError_t cfg1 = allow_dynamic_lds(dkdv, 2 * KEY_LDS_BYTES<D>);
     if (cfg1 != hipSuccess) return cfg1;
     hipLaunchKernelGGL(dq, dim3((unsigned)a.total_q), dim3(256), DQ_LDS_BYTES<D>, st, a);
-    hipLaunchKernelGGL(dkdv, dim3((unsigned)(a.far + a.total_k)), dim3(256), KEY_LDS_BYTES<D>, st, a);
+    hipLaunchKernelGGL(dkdv, dim3((unsigned)(a.far + a.total_k)), dim3(512), 2 * KEY_LDS_BYTES<D>, st, a);
     if (a.far > 0)
         hipLaunchKernelGGL(window_attention_sinks_kernel<D>, dim3((unsigned)(a.b.B * a.b.g * sinks_blocks(a.b.sinks, D))), dim3(256), 0, st, a);
     return hipGetLastError();

@@ -90,12 +90,12 @@ __device__ __forceinline__ int swz(int r) {
     else return ((r & 2) << 1) | ((r >> 2) & 3);
 }
 
-// Load of [TROWS x D] tiles of rows `ld` elements apart, 64 of them less than 4 GiB.  A wave fetches WROWS neighbouring rows, RPI with an
+// Load of [64 x D] tiles of rows `ld` elements apart, 64 of them less than 4 GiB.  Each of WAVES waves fetches WROWS neighbouring rows, RPI with an
 // instruction.  The instructions' swizzles differ from that of the first in two chunk bits; their offsets in memory and in LDS share the
 // immediate, so that one value of M0 serves them all.
-template <int D, int TROWS = BLK>
+template <int D, int WAVES = 4>
 struct TileLoad {
-    static constexpr int WROWS = TROWS / 4, RPI = 512 / D, PER = WROWS / RPI;
+    static constexpr int TROWS = BLK, WROWS = TROWS / WAVES, RPI = 512 / D, PER = WROWS / RPI;
     uint32_t voff, ld2, step;
     __device__ __forceinline__ TileLoad(int64_t ld, int wave) {
         const int lane = threadIdx.x & 63, rr = lane / (D / 8), c = lane % (D / 8);
@@ -178,6 +178,13 @@ __device__ __forceinline__ void load_fragments(half8 (&f)[D / 16], const uint16_
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) f[ks] = *reinterpret_cast<const half8*>(row + 16 * ks + 8 * lh);
 }
+// Waits for them.  Without it the compiler, which does not see the loads to LDS, waits where they are used, in every turn of a loop: for all that
+// is in flight there.
+template <int D>
+__device__ __forceinline__ void arrived(half8 (&f)[D / 16]) {
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(f[ks]));
+}
 
 // acc[i][r]: column 32 i + 8 (r / 4) + 4 lh + r % 4 of the lane's row, rounded once.  Every lane takes part in the exchange; `row` is null for
 // those that have no row.
@@ -200,10 +207,10 @@ __device__ __forceinline__ void store_rows(const floatx16 (&acc)[N], uint16_t* r
 // A product over a block that a mask cuts has zeros for the hidden pairs, and 0 * inf is not 0: the moving operand of such tiles is made
 // finite in LDS first.  What sees the values all the same gets to know of them otherwise: their rows' lse and delta are not finite,
 // and the forward adds them.  Each wave looks through the rows that it fetched; returned is one bit for each row that held any (uniform).
-template <int D, int TROWS = BLK>
+template <int D, int WAVES = 4>
 __device__ __forceinline__ uint32_t make_finite(uint32_t tile, int wave) {
     typedef __attribute__((address_space(3))) u32x4* chunk_p;
-    using Load = TileLoad<D, TROWS>;
+    using Load = TileLoad<D, WAVES>;
     constexpr int RPI = Load::RPI, LANES = 64 / RPI;      // of a row
     const int lane = threadIdx.x & 63;
     uint32_t rows = 0;

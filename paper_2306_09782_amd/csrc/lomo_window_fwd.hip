@@ -26,12 +26,11 @@ struct FwdArgs {
 
 }  // namespace win
 
-template <int D, int KEYS, int WAVES>
-__global__ __launch_bounds__(256, WAVES) void window_attention_forward_kernel(win::FwdArgs a) {
+template <int D>
+__global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::FwdArgs a) {
     using namespace win;
-    extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // two pairs of tiles of KEYS rows: K, V
+    extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // two pairs of tiles: K, V
     __shared__ uint32_t bad[2][4];                                        // rows of a V tile that are not finite, by wave
-    constexpr int HALVES = KEYS / 32, KTILE = KEYS * D, KPAIR = 2 * KTILE;
     constexpr float C2 = SCALE<D> * LOG2E;
 
     const int lane = threadIdx.x & 63;
@@ -59,21 +58,22 @@ __global__ __launch_bounds__(256, WAVES) void window_attention_forward_kernel(wi
     const uint16_t* gv = gk + (int64_t)a.b.g * D;
 
     // tiles of this workgroup: the sinks' where they are not among those of the window
-    const int first = max(0, q0 - window + 1) / KEYS, last = min(q0 + ROWS - 1, s.len - 1) / KEYS;
-    const int extra = min((sinks + KEYS - 1) / KEYS, first), tiles = last - first + 1 + extra;
+    const int first = max(0, q0 - window + 1) / BLK, last = min(q0 + ROWS - 1, s.len - 1) / BLK;
+    const int extra = min((sinks + BLK - 1) / BLK, first), tiles = last - first + 1 + extra;
     auto tile_at = [&](int i) { return i < extra ? i : first + i - extra; };
 
-    const TileLoad<D, KEYS> load(ld, wave);
+    const TileLoad<D> load(ld, wave);
     const TileRead<D> rd(lds0);
     auto fetch = [&](int tile, int buf) {
-        const uint32_t at = lds0 + (uint32_t)buf * (KPAIR * 2u);
-        load.issue(gk, tile, s.len - tile * KEYS, at, wave);
-        load.issue(gv, tile, s.len - tile * KEYS, at + KTILE * 2u, wave);
+        const uint32_t at = lds0 + (uint32_t)buf * (PAIR<D> * 2u);
+        load.issue(gk, tile, s.len - tile * BLK, at, wave);
+        load.issue(gv, tile, s.len - tile * BLK, at + TILE<D> * 2u, wave);
     };
     fetch(tile_at(0), 0);
 
     half8 fq[D / 16];
     if (active) load_fragments<D>(fq, gq + (int64_t)min(query, s.len - 1) * ld);
+    arrived<D>(fq);
 
     // log2 domain; l_run is this lane's share (its half of the keys)
     constexpr int NC = D / 32;
@@ -94,10 +94,10 @@ __global__ __launch_bounds__(256, WAVES) void window_attention_forward_kernel(wi
     // From scores to probabilities relative to the running maximum, in fp16.  The maximum moves only where it has grown by more than
     // SLACK: probabilities stay below 2^SLACK, and most tiles leave sum and output as they are.
     constexpr float SLACK = 8.f;
-    auto probabilities = [&](const floatx16 (&S)[HALVES], uint32_t (&pk)[HALVES][8]) {
+    auto probabilities = [&](const floatx16 (&S)[2], uint32_t (&pk)[2][8]) {
         float top = -INFINITY;
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, S[h][e]);
         const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256, WAVES) void window_attention_forward_kernel(wi
         const float m_ref = m_run == -INFINITY ? 0.f : m_run;      // a query that has seen no key yet
         float sum = 0.f;
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(fmaf(S[h][e], C2, -m_ref)), p1 = __builtin_amdgcn_exp2f(fmaf(S[h][e + 1], C2, -m_ref));
@@ -129,54 +129,54 @@ __global__ __launch_bounds__(256, WAVES) void window_attention_forward_kernel(wi
         // the tiles have landed; everybody is done with the other pair
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (it + 1 < tiles) fetch(tile_at(it + 1), (it + 1) & 1);      // in flight while this pair is multiplied
-        return rd.at((it & 1) * KPAIR);
+        return rd.at((it & 1) * PAIR<D>);
     };
     // o^T[column][query] += v^T[column][key] p^T[key][query], 16 keys at a time
-    auto values = [&](const TileRead<D>& r0, const uint32_t (&pk)[HALVES][8]) {
+    auto values = [&](const TileRead<D>& r0, const uint32_t (&pk)[2][8]) {
 #pragma unroll
-        for (int ks = 0; ks < 2 * HALVES; ++ks) {
+        for (int ks = 0; ks < 2 * 2; ++ks) {
             const half8 fp = fragment_of(pk[ks >> 1], ks & 1);
 #pragma unroll
-            for (int i = 0; i < NC; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.columns(KTILE, i, ks), fp, O[i], 0, 0, 0);
+            for (int i = 0; i < NC; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.columns(TILE<D>, i, ks), fp, O[i], 0, 0, 0);
         }
-        attn::interleave<8, 1, 2, 2 * HALVES * NC - 4, 4>();
+        attn::interleave<8, 1, 2, 2 * 2 * NC - 4, 4>();
     };
-    auto all_scores = [&](const TileRead<D>& r0, floatx16 (&S)[HALVES]) {
+    auto all_scores = [&](const TileRead<D>& r0, floatx16 (&S)[2]) {
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) scores(r0, h, S[h]);
-        attn::interleave<4, 1, 1, HALVES * D / 16 - 4, 4>();
+        for (int h = 0; h < 2; ++h) scores(r0, h, S[h]);
+        attn::interleave<4, 1, 1, 2 * D / 16 - 4, 4>();
     };
     // the tiles that every query of the workgroup sees whole
-    const int whole0 = (max(0, q0 + ROWS - window) + KEYS - 1) / KEYS, whole1 = q0 / KEYS - 1;
+    const int whole0 = (max(0, q0 + ROWS - window) + BLK - 1) / BLK, whole1 = q0 / BLK - 1;
     while (it < tiles) {
         for (; it < tiles && !(it >= extra && tile_at(it) >= whole0 && tile_at(it) <= whole1); ++it) {
-            const int k0 = tile_at(it) * KEYS;
+            const int k0 = tile_at(it) * BLK;
             const TileRead<D> r0 = begin();
-            const uint32_t mine = make_finite<D, KEYS>(lds0 + (uint32_t)(it & 1) * (KPAIR * 2u) + KTILE * 2u, wave);
+            const uint32_t mine = make_finite<D>(lds0 + (uint32_t)(it & 1) * (PAIR<D> * 2u) + TILE<D> * 2u, wave);
             if (lane == 0) bad[it & 1][wave] = mine;
             attn::meet();
             if (!active) continue;
             bool none = true;
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h) none = none && seen(qw, k0 + 32 * h, window, sinks) == NONE;
+            for (int h = 0; h < 2; ++h) none = none && seen(qw, k0 + 32 * h, window, sinks) == NONE;
             if (none) continue;
             // of a distance that is negative or not below the window, but for the sinks
             auto hidden = [&](int key) { return (uint32_t)(query - key) >= (key < sinks ? 0x80000000u : (uint32_t)window); };
-            floatx16 S[HALVES];
+            floatx16 S[2];
             all_scores(r0, S);
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     S[h][e] = hidden(k0 + 32 * h + 8 * (e >> 2) + 4 * lh + (e & 3)) ? -INFINITY : S[h][e];
                     if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
-            uint32_t pk[HALVES][8];
+            uint32_t pk[2][8];
             probabilities(S, pk);
             values(r0, pk);
             uint64_t rows = 0;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) rows |= (uint64_t)bad[it & 1][w] << (KEYS / 4 * w);
+            for (int w = 0; w < 4; ++w) rows |= (uint64_t)bad[it & 1][w] << (BLK / 4 * w);
             while (rows != 0) {      // what is not finite, to the queries that see its key
                 const int key = k0 + __builtin_ctzll(rows);
                 rows &= rows - 1;
@@ -195,9 +195,9 @@ __global__ __launch_bounds__(256, WAVES) void window_attention_forward_kernel(wi
         for (; it < tiles && tile_at(it) <= whole1; ++it) {
             const TileRead<D> r0 = begin();
             if (!active) continue;
-            floatx16 S[HALVES];
+            floatx16 S[2];
             all_scores(r0, S);
-            uint32_t pk[HALVES][8];
+            uint32_t pk[2][8];
             probabilities(S, pk);
             values(r0, pk);
         }
@@ -217,10 +217,10 @@ __global__ __launch_bounds__(256, WAVES) void window_attention_forward_kernel(wi
     if (own && lh == 0) a.lse[t * a.b.h + n] = (m_run + __builtin_amdgcn_logf(l)) * LN2;
 }
 
-template <int D, int KEYS, int WAVES>
+template <int D>
 static hipError_t launch_forward_of(const win::FwdArgs& a, hipStream_t st) {
-    auto kern = window_attention_forward_kernel<D, KEYS, WAVES>;
-    constexpr int lds = 2 * 2 * KEYS * D * 2;
+    auto kern = window_attention_forward_kernel<D>;
+    constexpr int lds = 2 * win::PAIR<D> * 2;
     static const hipError_t cfg = allow_dynamic_lds(kern, lds);
     if (cfg != hipSuccess) return cfg;
     hipLaunchKernelGGL(kern, dim3((unsigned)a.total), dim3(256), lds, st, a);
@@ -234,7 +234,7 @@ hipError_t launch_window_attention_forward(const uint16_t* qkv, uint16_t* o, flo
     a.qkv = qkv; a.o = o; a.lse = lse;
     a.numbers = (int)win::pieces(T, B, win::ROWS, 1);
     a.total = (int)(a.numbers * h);
-    return d == 128 ? launch_forward_of<128, 64, 2>(a, st) : launch_forward_of<64, 64, 2>(a, st);
+    return d == 128 ? launch_forward_of<128>(a, st) : launch_forward_of<64>(a, st);
 }
 
 }  // namespace lomo
