@@ -94,6 +94,11 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
     const uint16_t* row = a.z + t * a.V;
     uint16_t* out = a.dz + t * a.V;
     const int chunks = (int)(a.V >> 3);
+    // the listed columns of this thread: the first is on its way while the row arrives
+    auto listed = [&](int k) { return a.ids[t * a.K + k]; };
+    auto logit = [&](int k) { return (float)reinterpret_cast<const _Float16*>(a.teacher)[t * a.K + k]; };
+    int own = (int)threadIdx.x < a.K ? listed(threadIdx.x) : -1;
+    const float own_logit = (int)threadIdx.x < a.K ? logit(threadIdx.x) : 0.f;
     const int target = a.target[t];
     if (target < 0 || target >= a.V) {      // not counted
         if (threadIdx.x == 0) a.loss[t] = 0.f;
@@ -108,20 +113,13 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int c = i * NT + (int)threadIdx.x;
-            if (c < chunks) x[i] = *reinterpret_cast<const half8*>(row + (int64_t)c * 8);
+            if (c < chunks) x[i] = __builtin_nontemporal_load(reinterpret_cast<const half8*>(row + (int64_t)c * 8));
         }
     }
-    // the teacher's logits; an id outside [0, V) is not listed
-    float top = -INFINITY;
-    for (int k = threadIdx.x; k <= a.K; k += NT) {
-        const int i = k < a.K ? a.ids[t * a.K + k] : target;
-        const bool in = i >= 0 && i < a.V;
-        const float l = k < a.K && in ? (float)reinterpret_cast<const _Float16*>(a.teacher)[t * a.K + k] / a.tau : -INFINITY;
-        id[k] = in ? i : -1;
-        zk[k] = in ? (float)reinterpret_cast<const _Float16*>(row)[i] : 0.f;      // before anything is overwritten
-        p[k] = l;
-        top = fmaxf(top, l);
-    }
+    // the student's logit of a listed column, read before anything is overwritten; an id outside [0, V) is not listed
+    auto column = [&](int i) { return i >= 0 && i < a.V ? (float)reinterpret_cast<const _Float16*>(row)[i] : 0.f; };
+    if ((int)threadIdx.x == a.K) own = target;
+    const float own_z = column(own);
     constexpr float LOWEST = -65504.f;      // finite from the start: masked logits may be -inf
     float m0 = LOWEST;
     if (CH > 0 && (int)threadIdx.x < chunks) m0 = fmaxf(m0, largest(x[0]));
@@ -134,6 +132,19 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
         }
     } else {
         for (int c = threadIdx.x; c < chunks; c += NT) s.add(*reinterpret_cast<const half8*>(row + (int64_t)c * 8), ch, cs);
+    }
+    float top = -INFINITY;
+    auto keep = [&](int k, int i, float z, float l) {
+        const bool in = i >= 0 && i < a.V;
+        p[k] = k < a.K && in ? l / a.tau : -INFINITY;
+        zk[k] = z;
+        id[k] = in ? i : -1;
+        top = fmaxf(top, p[k]);
+    };
+    if ((int)threadIdx.x <= a.K) keep(threadIdx.x, own, own_z, own_logit);
+    for (int k = threadIdx.x + NT; k <= a.K; k += NT) {
+        const int i = k < a.K ? listed(k) : target;
+        keep(k, i, column(i), k < a.K ? logit(k) : 0.f);
     }
     {
         const float m = wave_max(s.m);
@@ -194,14 +205,16 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int c = i * NT + (int)threadIdx.x;
-            if (c < chunks) *reinterpret_cast<half8*>(out + (int64_t)c * 8) = gradient(x[i]);
+            if (c < chunks) __builtin_nontemporal_store(gradient(x[i]), reinterpret_cast<half8*>(out + (int64_t)c * 8));
             __builtin_amdgcn_sched_barrier(0);
         }
     } else {
         for (int c = threadIdx.x; c < chunks; c += NT)
             *reinterpret_cast<half8*>(out + (int64_t)c * 8) = gradient(*reinterpret_cast<const half8*>(row + (int64_t)c * 8));
     }
-    __syncthreads();      // p is whole, the row is written; what follows replaces some of it
+    // p is whole, and every wave's part of the row is where other waves' stores find it: what follows replaces some of it
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
     const float sum = wave_sum(has ? red[3][lane] : 0.f);
     if (threadIdx.x == 0) {
         float l = w > 0.f ? w * a.tau * a.tau * sum : 0.f;
