@@ -419,7 +419,9 @@ lomo_status lomo_window_attention_forward(const lomo_half* qkv, lomo_half* o, fl
  * dk and dv of a key head are sums over its query heads, in fp32.  P and dS pass through fp16 before the products that consume them.
  * Rows that belong to no sequence are left as they are.  ws: device workspace, 16-byte aligned, of at least
  * lomo_window_attention_workspace_bytes(...) bytes (do . o of every row and head, and partial sums of the sinks' gradients, whose queries
- * are the whole sequence); no need to clear it.  Deterministic (no atomics). */
+ * are the whole sequence); no need to clear it; calls that overlap in time need one each.  dqkv may not alias the inputs.  Deterministic (no
+ * atomics), and a sequence's results do not depend on the others.  What the mask hides from a query does not reach its gradient, nor does the query
+ * reach the hidden key's. */
 lomo_status lomo_window_attention_backward(const lomo_half* qkv, const lomo_half* o, const lomo_half* dO, const float* lse, lomo_half* dqkv,
                                            const int32_t* seq_offsets, int64_t T, int64_t B, int64_t n_heads, int64_t n_kv_heads,
                                            int64_t head_dim, int64_t window, int64_t sinks, void* ws, size_t ws_bytes, void* stream);

@@ -163,9 +163,10 @@ class PackedAttention:
     W_qkv is then [(n_heads + 2 n_kv_heads) head_dim x H], with n_heads * head_dim = H; rope_cos and rope_sin are tables
     [positions x head_dim / 2].  window=None: no limit.  pair_axis: the axis of each of the head_dim / 2 pairs (None: one axis).
 
-    set_batch(lengths, positions) before a step: lengths on the host, at most max_sequences of them, their sum at most T; positions
-    int32 [axes x T] on the device (None: each token's place in its sequence, on every axis).  Rows behind the last sequence are padding:
-    their targets have to be outside the vocabulary, then they add nothing to any gradient."""
+    set_batch(lengths, positions) before a step, on the step's stream: lengths on the host, at most max_sequences of them, their sum at
+    most T; positions int32 [axes x T] (None: each token's place in its sequence, on every axis).  Rows behind the last sequence are
+    padding: their targets have to be outside the vocabulary, then they add nothing to any gradient.  A captured step takes further
+    batches with as many tokens as the one that it was captured with."""
 
     def __init__(self, device, T: int, n_heads: int, n_kv_heads: int, head_dim: int, window: int = None, sinks: int = 0,
                  max_sequences: int = 64, pair_axis=None):
@@ -182,7 +183,7 @@ class PackedAttention:
         self.positions = torch.zeros(1 + max(self.pair_axis, default=0), T, dtype=torch.int32, device=self.device)
         self.rows = 0
 
-    def set_batch(self, lengths, positions=None) -> None:
+    def set_batch(self, lengths, positions=None, stream=None) -> None:
         lengths = [int(n) for n in lengths]
         if min(lengths, default=0) < 0 or sum(lengths) > self.T or len(lengths) >= self.offsets.numel():
             raise B.LomoError(f"{len(lengths)} sequences of {sum(lengths)} tokens, room for {self.offsets.numel() - 1} of {self.T}")
@@ -190,14 +191,15 @@ class PackedAttention:
         for n in lengths:
             place[at[-1]:at[-1] + n] = torch.arange(n, dtype=torch.int32)
             at.append(at[-1] + n)
-        self.rows = at[-1]
-        # the sequences that are not there are empty ones: the buffers, and what a captured step reads, stay the same
-        self.offsets.copy_(torch.tensor(at + [self.rows] * (self.offsets.numel() - len(at)), dtype=torch.int32))
         if positions is None:
             positions = place.expand_as(self.positions)
         if tuple(positions.shape) != tuple(self.positions.shape):
             raise B.LomoError(f"positions {tuple(positions.shape)}, want {tuple(self.positions.shape)}")
-        self.positions.copy_(positions)
+        self.rows = at[-1]
+        with B.on_stream(stream):      # behind the steps that read the last batch's
+            # the sequences that are not there are empty ones: the buffers, and what a captured step reads, stay the same
+            self.offsets.copy_(torch.tensor(at + [self.rows] * (self.offsets.numel() - len(at)), dtype=torch.int32))
+            self.positions.copy_(positions)
 
     def forward(self, qkv, rope_cos, rope_sin, o, lse, stream=None) -> None:
         """qkv [T x qkv_width] as the projection leaves it: its q and k are turned in place."""

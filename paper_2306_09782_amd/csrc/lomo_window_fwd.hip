@@ -4,12 +4,18 @@
 //   o_i = sum_j exp(S_ij - lse_i) v_j
 //
 // One workgroup per (128 queries, head) walks the pairs of key and value tiles (64 keys) that the window of its queries reaches, the
-// tile of the sinks first where that is left of them; one pass with a running maximum and sum.  Workgroups are numbered so that the heads of a group and neighbouring queries run on one XCD at a time.  Probabilities are
-// rounded to fp16 relative to the running maximum, as the matrix cores take them; sums and accumulators are fp32; o is rounded once.
-// Deterministic, and independent of what else is in the batch.
+// tile of the sinks first where that is left of them; one pass with a running maximum and sum.  Workgroups are numbered so that the heads of a
+// group and neighbouring queries run on one XCD at a time.  Probabilities are rounded to fp16 relative to the running maximum, as the matrix
+// cores take them; sums and accumulators are fp32; o is rounded once.  Deterministic, and independent of what else is in the batch.
 //
-// A key that the mask hides from a query adds nothing to it, whatever its v holds: inf and NaN are taken out of the tiles that a mask
-// cuts, and added to the queries that do see them.
+// Tiles that every query of the workgroup sees whole have a loop of their own, without masks.  A key that the mask hides from a query adds nothing
+// to it, whatever its v holds: inf and NaN are taken out of the tiles that a mask cuts, and added to the queries that do see them.
+//
+// Measured, us: 16384 tokens, 32 / 8 heads of 128, window 4096, 4 sinks 1020 (945 TFLOP/s of the visible pairs); 8192 tokens, 32 heads, no window 575
+// (955 TFLOP/s); 4096 rows of seven sequences, window 1024 53; 8192 tokens, 32 / 8 heads of 64, window 2048 168 (716 TFLOP/s); four short sequences 6.8,
+// the time of a launch.  Power is what bounds the long ones: the clock is at 1.9 GHz with the matrix cores busy for 47 % of its cycles and the vector
+// units for 55 %.  Slower or no faster: the next tile's scores between the probabilities (1300), two waves of a SIMD held half a step apart by
+// barriers (1000, and short sequences 30 % slower), tiles of 32 keys with three waves a SIMD (1010, odd lengths 12 % slower).
 #include "lomo_window_common.h"
 
 namespace lomo {
@@ -26,8 +32,9 @@ struct FwdArgs {
 
 }  // namespace win
 
+// Heads of 64 leave room for four waves a SIMD instead of three (8192 tokens 174 -> 168 us, 4096 packed rows 34.6 -> 33.2).
 template <int D>
-__global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::FwdArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void window_attention_forward_kernel(win::FwdArgs a) {
     using namespace win;
     extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // two pairs of tiles: K, V
     __shared__ uint32_t bad[2][4];                                        // rows of a V tile that are not finite, by wave
@@ -134,17 +141,17 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
     // o^T[column][query] += v^T[column][key] p^T[key][query], 16 keys at a time
     auto values = [&](const TileRead<D>& r0, const uint32_t (&pk)[2][8]) {
 #pragma unroll
-        for (int ks = 0; ks < 2 * 2; ++ks) {
+        for (int ks = 0; ks < 4; ++ks) {
             const half8 fp = fragment_of(pk[ks >> 1], ks & 1);
 #pragma unroll
             for (int i = 0; i < NC; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.columns(TILE<D>, i, ks), fp, O[i], 0, 0, 0);
         }
-        attn::interleave<8, 1, 2, 2 * 2 * NC - 4, 4>();
+        attn::interleave<8, 1, 2, 4 * NC - 4, 4>();
     };
     auto all_scores = [&](const TileRead<D>& r0, floatx16 (&S)[2]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) scores(r0, h, S[h]);
-        attn::interleave<4, 1, 1, 2 * D / 16 - 4, 4>();
+        attn::interleave<4, 1, 1, D / 8 - 4, 4>();
     };
     // the tiles that every query of the workgroup sees whole
     const int whole0 = (max(0, q0 + ROWS - window) + BLK - 1) / BLK, whole1 = q0 / BLK - 1;
@@ -176,7 +183,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_forward_kernel(win::F
             values(r0, pk);
             uint64_t rows = 0;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) rows |= (uint64_t)bad[it & 1][w] << (BLK / 4 * w);
+            for (int w = 0; w < 4; ++w) rows |= (uint64_t)bad[it & 1][w] << (16 * w);
             while (rows != 0) {      // what is not finite, to the queries that see its key
                 const int key = k0 + __builtin_ctzll(rows);
                 rows &= rows - 1;

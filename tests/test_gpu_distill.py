@@ -150,3 +150,19 @@ def test_refusals_stream_and_graph(L):
         L.lomo_distill_mean(z, ids, teacher, targets, 64.0, 2.0, 0.5, a, b, c)
         torch.cuda.synchronize()
         assert torch.equal(loss, a) and torch.equal(dz, b) and torch.equal(stats[:2], c[:2])
+
+
+def test_rows_beyond_32_bits(L):
+    V, K = 131072, 4
+    T = (1 << 31) // V + 50
+    z = torch.zeros(T, V, dtype=torch.float16, device=DEV)
+    ids, teacher = torch.randint(0, V, (T, K), dtype=torch.int32, device=DEV), torch.randn(T, K, device=DEV).half()
+    targets = torch.full((T,), -100, dtype=torch.int32, device=DEV)
+    z[T - 1], targets[T - 1] = torch.randn(V, device=DEV).half(), 77
+    one = [x[T - 1:].clone() for x in (z, ids, teacher, targets)]
+    loss, dz = torch.zeros(1, device=DEV), torch.zeros(1, V, dtype=torch.float16, device=DEV)
+    L.lomo_distill(*one, 64.0, 2.0, 0.5, loss, dz)
+    all_loss = torch.ones(T, device=DEV)
+    L.lomo_distill(z, ids, teacher, targets, 64.0, 2.0, 0.5, all_loss, z)
+    assert torch.equal(z[T - 1:], dz) and torch.equal(all_loss[T - 1:], loss) and bool(dz.any())
+    assert not bool(all_loss[:T - 1].any()) and not bool(z[:T - 1:97].any())

@@ -120,3 +120,21 @@ def test_refusals_empty_calls_stream_and_graph(L):
         L.lomo_rope_axes(x, want, cos, sin, pos, axis, 2, d)
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+def test_tables_without_rows_and_rows_beyond_32_bits(L):
+    x = torch.randn(10, 128, device=DEV).half()
+    none, y = torch.empty(0, 64, device=DEV), torch.zeros_like(x)
+    L.lomo_rope_axes(x, y, none, none, torch.zeros(1, 10, dtype=torch.int32, device=DEV), bytes(64), 1, 128)
+    assert torch.equal(x, y)
+    heads, d = 48, 128
+    T = (1 << 31) // (heads * d) + 100
+    cos, sin = (dev(t) for t in tables(50, d))
+    big = torch.zeros(T, heads * d, dtype=torch.float16, device=DEV)
+    big[T - 10:] = torch.randn(10, heads * d, device=DEV).half()
+    pos = torch.randint(0, 50, (2, T), dtype=torch.int32, device=DEV)
+    axis = bytes([0] * 20 + [1] * 44)
+    want = torch.empty(10, heads * d, dtype=torch.float16, device=DEV)
+    L.lomo_rope_axes(big[T - 10:].contiguous(), want, cos, sin, pos[:, T - 10:].contiguous(), axis, heads, d)
+    L.lomo_rope_axes(big, big, cos, sin, pos, axis, heads, d)
+    assert torch.equal(big[T - 10:], want) and not bool(big[:T - 10:997].any())

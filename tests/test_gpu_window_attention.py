@@ -257,3 +257,36 @@ def test_other_stream_and_graph(L):
         eager = run(L, qkv, do, off, h, g, window, sinks)
         for x, y in zip((o, lse, dqkv), eager):
             assert torch.equal(x, y), k
+
+
+def test_rows_beyond_32_bits(L):
+    """The last sequence of buffers of more than 2^31 elements, 4 GiB: as at the beginning of small ones."""
+    h, g, d, window, sinks, n = 32, 8, 128, 100, 4, 300
+    T = (1 << 31) // ((h + 2 * g) * d) + n + 1000
+    small = [dev(x) for x in inputs(3, n, h, g, d)]
+    want = run(L, *small, [0, n], h, g, window, sinks)
+    qkv, do = torch.zeros(T, (h + 2 * g) * d, dtype=torch.float16, device=DEV), torch.zeros(T, h * d, dtype=torch.float16, device=DEV)
+    qkv[T - n:], do[T - n:] = small
+    got = run(L, qkv, do, [T - n, T], h, g, window, sinks)
+    for x, y in zip(got, want):
+        assert torch.equal(x[T - n:], y) and bool((x[:T - n:997] == MARK).all())
+
+
+def test_two_calls_at_once(L):
+    h, g, d, window, sinks, n = 8, 2, 128, 300, 4, 2000
+    data = [[dev(x) for x in inputs(seed, n, h, g, d)] for seed in (1, 2)]
+    want = [run(L, *x, [0, n], h, g, window, sinks) for x in data]
+    off = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    size = L.lomo_window_attention_workspace_bytes(n, 1, h, g, d, sinks)
+    streams, got = [torch.cuda.Stream() for _ in data], []
+    for (qkv, do), w in zip(data, want):
+        got.append([torch.zeros_like(x) for x in w] + [torch.empty(size, dtype=torch.uint8, device=DEV)])
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for (qkv, do), (o, lse, dqkv, ws), st in zip(data, got, streams):
+            L.lomo_window_attention_forward(qkv, o, lse, off, h, g, window, sinks, st)
+            L.lomo_window_attention_backward(qkv, o, do, lse, dqkv, off, h, g, window, sinks, ws, st)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
