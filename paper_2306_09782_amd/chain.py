@@ -181,7 +181,7 @@ class PackedAttention:
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self.offsets = torch.zeros(max_sequences + 1, dtype=torch.int32, device=self.device)
         self.positions = torch.zeros(1 + max(self.pair_axis, default=0), T, dtype=torch.int32, device=self.device)
-        self.rows = 0
+        self.rows = None             # of the batch's sequences, from set_batch()
 
     def set_batch(self, lengths, positions=None, stream=None) -> None:
         lengths = [int(n) for n in lengths]
@@ -203,6 +203,8 @@ class PackedAttention:
 
     def forward(self, qkv, rope_cos, rope_sin, o, lse, stream=None) -> None:
         """qkv [T x qkv_width] as the projection leaves it: its q and k are turned in place."""
+        if self.rows is None:
+            raise B.LomoError("no batch: set_batch() comes before the step")
         B.lomo_rope_axes(qkv, qkv, rope_cos, rope_sin, self.positions, self.pair_axis, self.n_heads + self.n_kv_heads, self.head_dim,
                          stream=stream)
         B.lomo_window_attention_forward(qkv, o, lse, self.offsets, self.n_heads, self.n_kv_heads, self.window, self.sinks, stream)

@@ -16,11 +16,13 @@ inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) &
 inline lomo_status from_hip(hipError_t e) { return e == hipSuccess ? LOMO_OK : LOMO_ERR_LAUNCH; }
 inline bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 
+constexpr int64_t MAX_THREADS = 0xffffffff;      // of one dimension of a launch
+
 // What the calls on packed sequences ask of their sizes.
 inline bool window_sizes_ok(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks) {
     if (T < 0 || B < 0 || h <= 0 || g <= 0 || h % g != 0 || (d != 64 && d != 128) || sinks < 0 || sinks > 64) return false;
     if (T > (1 << 30) || B > (1 << 24) || h > (1 << 16)) return false;      // with this, 64 rows stay below 4 GiB
-    return window_attention_grid(T, B, h, g, d, sinks) <= 0x7fffffff;
+    return window_attention_threads(T, B, h, g, d, sinks) <= MAX_THREADS;
 }
 inline float step_size(float lr, float inv_loss_scale, float clip_coef) {
     return (float)((double)lr * (double)clip_coef * (double)inv_loss_scale);
@@ -701,7 +703,7 @@ lomo_status lomo_rope_axes(const lomo_half* x, int64_t ldx, lomo_half* y, int64_
                            int64_t n_heads, int64_t head_dim, int inverse, void* stream) {
     if (T < 0 || n_positions < 0 || n_axes < 1 || n_axes > 8 || n_heads < 0 || head_dim < 16 || head_dim > 256 || (head_dim & 15))
         return LOMO_ERR_SHAPE;
-    if (T > 0x7fffffff || n_heads > (1 << 16) || (ldx & 7) || (ldy & 7) || ldx < n_heads * head_dim || ldy < n_heads * head_dim || (x == y && ldx != ldy))
+    if (T > 0x7fffffff || T * (head_dim / 16) > MAX_THREADS - 256 || n_heads > (1 << 16) || (ldx & 7) || (ldy & 7) || ldx < n_heads * head_dim || ldy < n_heads * head_dim || (x == y && ldx != ldy))
         return LOMO_ERR_SHAPE;
     if (!pair_axis) return LOMO_ERR_NULL;
     for (int64_t c = 0; c < head_dim / 2; ++c)
@@ -753,8 +755,9 @@ lomo_status lomo_window_attention_backward(const lomo_half* qkv, const lomo_half
 // What lomo_distill and lomo_distill_mean ask of what they share.
 static lomo_status distill_arguments(const lomo_half* logits, const int32_t* ids, const lomo_half* teacher, const int32_t* targets,
                                      float temperature, float soft_weight, float* loss, lomo_half* dlogits, int64_t T, int64_t V, int64_t K) {
-    if (T < 0 || V < 0 || (V & 7) || T > 0x7fffffff || V > 0x7fffffff || K < 1 || K > 1024) return LOMO_ERR_SHAPE;
-    if (!(temperature > 0.f) || !isfinite(temperature) || !(soft_weight >= 0.f && soft_weight <= 1.f)) return LOMO_ERR_SHAPE;
+    if (T < 0 || V < 0 || (V & 7) || T > MAX_THREADS / 1024 || V > 0x7fffffff || K < 1 || K > 1024) return LOMO_ERR_SHAPE;
+    // fp32 exponents of z / tau stay meaningful in between for every fp16 z
+    if (!(temperature >= 1.f / 1024 && temperature <= 1024.f) || !(soft_weight >= 0.f && soft_weight <= 1.f)) return LOMO_ERR_SHAPE;
     if (T == 0) return LOMO_OK;
     if (V == 0) return LOMO_ERR_SHAPE;
     if (!logits || !ids || !teacher || !targets || !loss || !dlogits) return LOMO_ERR_NULL;

@@ -13,7 +13,7 @@
 //
 // fp32 accumulation on the matrix cores.  P and dS pass through fp16 before the products that consume them; P is held times 2^15 there,
 // so that the probabilities of a long window (2^-14 and less) keep all their bits.  dq, dk, dv are rounded once.  Tiles that a mask cuts are
-// made finite first, so that a pair which the mask hides adds nothing.
+// made finite first, so that a pair which the mask hides adds nothing; a query that sees a key which is not finite has NaN in its gradient.
 //
 // Measured, us: 16384 tokens, 32 / 8 heads of 128, window 2048, 4 sinks 2200 (dq 800, dk and dv 1390; 585 TFLOP/s of the five products, 820 of
 // the seven executed); 4096 rows of seven sequences, window 1024 187; four short sequences 25.  The matrix cores are busy for 34 to 45 % of
@@ -198,6 +198,7 @@ template <int D>
 __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArgs a) {
     using namespace win;
     extern __shared__ __attribute__((aligned(256))) uint16_t smem[];      // two pairs of tiles: K, V
+    __shared__ uint32_t bad[2][4];                                        // rows of a K tile that are not finite, by wave
     constexpr float C2 = SCALE<D> * LOG2E;
 
     const int lane = threadIdx.x & 63;
@@ -254,8 +255,9 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
     floatx16 acc[D / 32];
     clear(acc);
 
-    // dS of keys k0 .. k0 + 31 as fragments
-    auto gradients = [&](const TileRead<D>& r0, int k0, auto cut, half8 (&f)[2]) {
+    // dS of keys k0 .. k0 + 31 as fragments.  Bits of `rows`: keys that are not finite; a query that sees one has an lse and a delta that are not,
+    // unless its score is -inf: then P is 0 and dS times the key is NaN in its infinite columns.
+    auto gradients = [&](const TileRead<D>& r0, int k0, auto cut, uint32_t rows, half8 (&f)[2]) {
         floatx16 S, P;
         products<D>(r0, fq, fd, S, P);
         uint32_t pk[8];
@@ -271,6 +273,11 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
                 S[e] = h ? 0.f : p;
                 P[e] = h ? 0.f : d;
             }
+        }
+        if (decltype(cut)::value && rows != 0) {
+            const uint32_t own = rows >> (4 * lh);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S[e] = own >> (8 * (e >> 2) + (e & 3)) & 1 ? 0.f : S[e];
         }
 #pragma unroll
         for (int e = 0; e < 16; e += 2) pk[e >> 1] = pack2(S[e] * P[e], S[e + 1] * P[e + 1]);
@@ -292,16 +299,32 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
         for (; it < tiles && !(it >= extra && tile_at(it) >= whole0 && tile_at(it) <= whole1); ++it) {
             const int k0 = tile_at(it) * BLK;
             const TileRead<D> r0 = begin();
-            make_finite<D>(lds0 + (uint32_t)(it & 1) * (PAIR<D> * 2u), wave);
+            const uint32_t mine = make_finite<D>(lds0 + (uint32_t)(it & 1) * (PAIR<D> * 2u), wave);
+            if (lane == 0) bad[it & 1][wave] = mine;
             attn::meet();
             if (!active) continue;
 #pragma nounroll
             for (int h = 0; h < 2; ++h) {
                 if (seen(qw, k0 + 32 * h, window, sinks) == NONE) continue;
                 const TileRead<D> r1 = r0.at(32 * h * D);
+                uint32_t rows = __builtin_amdgcn_readfirstlane(bad[it & 1][2 * h] | bad[it & 1][2 * h + 1] << 16);
                 half8 f[2];
-                gradients(r1, k0 + 32 * h, std::true_type{}, f);
+                gradients(r1, k0 + 32 * h, std::true_type{}, rows, f);
                 multiply<D>(r1, 0, f, acc);
+                while (rows != 0) {      // what is not finite of a key, to the queries that see it
+                    const int key = k0 + 32 * h + __builtin_ctz(rows);
+                    rows &= rows - 1;
+                    if (key > query || (query - key >= window && key >= sinks)) continue;
+                    const uint16_t* k = gk + (int64_t)key * ld + 4 * lh;
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                        for (int g4 = 0; g4 < 4; ++g4) {
+                            const half4 x = *reinterpret_cast<const half4*>(k + 32 * i + 8 * g4);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][4 * g4 + e] += not_finite((float)x[e]) ? NAN : 0.f;
+                        }
+                }
             }
         }
         for (; it < tiles && tile_at(it) <= whole1; ++it) {
@@ -311,7 +334,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
             for (int h = 0; h < 2; ++h) {
                 const TileRead<D> r1 = r0.at(32 * h * D);
                 half8 f[2];
-                gradients(r1, 0, std::false_type{}, f);
+                gradients(r1, 0, std::false_type{}, 0u, f);
                 multiply<D>(r1, 0, f, acc);
             }
         }
@@ -517,10 +540,11 @@ __global__ __launch_bounds__(256) void window_attention_sinks_kernel(win::BwdArg
     a.dqkv[((int64_t)s.start + row) * (a.b.h + 2 * a.b.g) * D + (int64_t)(a.b.h + which * a.b.g + kv) * D + c] = __builtin_bit_cast(uint16_t, x);
 }
 
-int64_t window_attention_grid(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks) {
+// Threads of the largest launch.
+int64_t window_attention_threads(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks) {
     using namespace win;
     const int64_t rows = pieces(T, B, ROWS, 1) * h, keys = (pieces(T, B, BLK, 1) + pieces(T, B, FAR_ROWS, 2)) * g;
-    return std::max(std::max(rows, keys), B * g * sinks_blocks((int)sinks, (int)d));
+    return std::max(std::max(256 * rows, 512 * keys), 256 * B * g * sinks_blocks((int)sinks, (int)d));
 }
 size_t window_attention_delta_bytes(int64_t T, int64_t h) { return ((size_t)T * h * 4 + 255) & ~(size_t)255; }
 size_t window_attention_ws_bytes(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks) {

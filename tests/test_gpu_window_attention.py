@@ -194,6 +194,41 @@ def test_one_infinite_value_reaches_its_column_alone(L):
     assert bool((o.view(n, h, d)[50:90, :, 9] == float("inf")).all()) and bool(lse.isfinite().all())
 
 
+@pytest.mark.parametrize("n,window,sinks,key", [(300, 90, 2, 0), (300, 90, 2, 131), (700, 5000, 0, 70), (60, 60, 0, 5)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradient_of_queries_that_score_minus_infinity(L, d, n, window, sinks, key):
+    """A key with one infinite element: queries whose score is -inf have a finite lse, P = 0 there, and 0 * inf = NaN in that column of dq alone;
+    the others meet +inf and have nothing finite."""
+    h, g, col = 2, 1, 9
+    qkv, do = inputs(n + key, n, h, g, d)
+    qkv[:, col] = -np.abs(qkv[:, col]) - np.float16(0.1)      # head 0 scores -inf
+    qkv[:, d + col] = np.abs(qkv[:, d + col]) + np.float16(0.1)
+    finite = qkv.copy()
+    qkv[key, h * d + col] = np.inf
+    o, lse, dqkv = run(L, dev(qkv), dev(do), [0, n], h, g, window, sinks)
+    see = S.visible(n, window, sinks)
+    hit = see[:, key]
+    dq = dqkv.view(n, h + 2 * g, d)[:, :h].float().cpu().numpy()
+    want = np.ones((n, d), bool)
+    want[hit, col] = False
+    got = np.isfinite(dq[:, 0])
+    rows = np.arange(n) != (0 if key == 0 else -1)      # a query that sees nothing else has no lse, and nothing finite
+    np.testing.assert_array_equal(got[rows], want[rows])
+    assert not np.isfinite(dq[hit, 1]).any() and np.isfinite(dq[~hit, 1]).all()
+    # the finite entries of head 0, with the key's share taken out
+    q, v, u = (x.astype(np.float64) for x in (finite[:, :d], finite[:, (h + g) * d:], do[:, :d]))
+    k = finite[:, h * d:(h + 1) * d].astype(np.float64)
+    w, e = o[:, :d].cpu().numpy().astype(np.float64), lse[:, 0].cpu().numpy().astype(np.float64)
+    left = see.copy()
+    left[:, key] = False
+    with np.errstate(all="ignore"):
+        p = np.where(left, np.exp(q @ k.T / d ** 0.5 - e[:, None]), 0.0)
+        grad = (p * (u @ v.T - (u * w).sum(1, keepdims=True)) / d ** 0.5) @ k
+        _, bound = S.window_attention_backward(finite, o.cpu().numpy(), do, lse.cpu().numpy(), [0, n], h, g, window, sinks)
+    ok = want & rows[:, None]
+    assert (np.abs(dq[:, 0] - grad)[ok] <= bound[:, :d][ok]).all()
+
+
 def test_offsets_that_do_not_ascend_stay_in_bounds(L):
     """No results are promised; rows before and behind the buffers' own are not touched."""
     h, g, d, T = 2, 1, 64, 300

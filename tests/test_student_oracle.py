@@ -171,3 +171,25 @@ def test_binding_refuses_what_it_cannot_pass_on():
         L.lomo_window_attention_forward(half(4, 384), half(4, 128), single(4, 1), whole(2), 1, 1, 4)
     with pytest.raises(L.LomoError, match="current device"):
         L.lomo_distill(half(4, 16), whole(4, 2), half(4, 2), whole(4), 1.0, 1.0, 0.5, single(4), half(4, 16))
+
+
+def test_refusals_of_what_no_launch_holds(lib):
+    """Launches of 2^32 threads and more, temperatures at which fp32 exponents of fp16 logits mean nothing: before anything is launched."""
+    window = lib.lomo_window_attention_forward
+    assert window(A16, A16, A16, A16, 100, 1 << 24, 4, 2, 128, 8, 4, P) == SHAPE
+    assert lib.lomo_window_attention_workspace_bytes(100, 1 << 24, 4, 2, 128, 4) == 0
+    assert lib.lomo_rope_axes(A16, 256, A16, 256, A16, A16, 4, A16, 1, bytes(128), 1 << 28, 1, 256, 0, P) == SHAPE
+    for tau, T in ((2.0 ** -11, 4), (2.0 ** 11, 4), (1.0, 1 << 22)):
+        assert lib.lomo_distill(A16, A16, A16, A16, 1.0, tau, 0.5, A16, A16, T, 16, 3, P) == SHAPE
+        assert lib.lomo_distill_mean(A16, A16, A16, A16, 1.0, tau, 0.5, A16, A16, A16, T, 16, 3, P) == SHAPE
+
+
+def test_packed_attention_wants_a_batch_first(lib):
+    from paper_2306_09782_amd.chain import PackedAttention
+    packed = PackedAttention("cpu", 10, 2, 1, 64, window=4)
+    half = lambda *s: torch.zeros(*s, dtype=torch.float16)
+    with pytest.raises(L.LomoError, match="set_batch"):
+        packed.forward(half(10, 256), torch.zeros(10, 32), torch.zeros(10, 32), half(10, 128), torch.zeros(10, 2))
+    for lengths in ([11], [5, -1], [1] * 65):
+        with pytest.raises(L.LomoError, match="sequences"):
+            packed.set_batch(lengths)
