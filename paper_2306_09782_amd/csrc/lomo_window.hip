@@ -15,11 +15,13 @@
 // so that the probabilities of a long window (2^-14 and less) keep all their bits.  dq, dk, dv are rounded once.  Tiles that a mask cuts are
 // made finite first, so that a pair which the mask hides adds nothing; a query that sees a key which is not finite has NaN in its gradient.
 //
-// Measured, us: 16384 tokens, 32 / 8 heads of 128, window 2048, 4 sinks 2200 (dq 800, dk and dv 1390; 585 TFLOP/s of the five products, 820 of
-// the seven executed); 4096 rows of seven sequences, window 1024 187; four short sequences 25.  The matrix cores are busy for 34 to 45 % of
-// the cycles of a clock that power holds at 2.0 GHz.  A packed batch is bound by its longest walk: the two teams of a workgroup took it from 206
-// to 187 (short 29 -> 25; 16384 tokens, where there are walks enough, 2090 -> 2200).  128 keys to a workgroup, dk and dv in one wave: 2060, but 222 and
-// 29.  Without the meeting of partners 1 % less, without exponentials 1 %.
+// Measured, us: 16384 tokens, 32 / 8 heads of 128, window 2048, 4 sinks 2190 (dq 800, dk and dv 1390; 588 TFLOP/s of the five products, 820 of
+// the seven executed); 4096 rows of seven sequences, window 1024 189; four short sequences 25.  Power bounds the long ones: the clock falls below
+// 2.0 GHz with the matrix cores busy for half (dq) and a third (dk, dv) of its cycles, and what takes stalls away changes nothing: three pairs of
+// tiles in flight, one barrier a tile with the partner's half multiplied beside the next scores, no exponentials (1 %), no meeting of partners
+// (1 %).  Fewer bytes do: without tile loads 18 % of dk and dv less.  A packed batch is bound by its longest walk: the two teams of a workgroup
+// took it from 206 to 189 (short 29 -> 25; 16384 tokens, where there are walks enough, 2090 -> 2190).  Both teams on 128 keys and the same tiles:
+// 2065, but 222 and 30; by the size of a call it would make a sequence's bits depend on its batch.
 #include "lomo_window_common.h"
 
 #include <algorithm>

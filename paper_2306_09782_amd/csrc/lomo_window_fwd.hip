@@ -11,9 +11,9 @@
 // Tiles that every query of the workgroup sees whole have a loop of their own, without masks.  A key that the mask hides from a query adds nothing
 // to it, whatever its v holds: inf and NaN are taken out of the tiles that a mask cuts, and added to the queries that do see them.
 //
-// Measured, us: 16384 tokens, 32 / 8 heads of 128, window 4096, 4 sinks 1020 (945 TFLOP/s of the visible pairs); 8192 tokens, 32 heads, no window 575
+// Measured, us: 16384 tokens, 32 / 8 heads of 128, window 4096, 4 sinks 1025 (940 TFLOP/s of the visible pairs); 8192 tokens, 32 heads, no window 575
 // (955 TFLOP/s); 4096 rows of seven sequences, window 1024 53; 8192 tokens, 32 / 8 heads of 64, window 2048 168 (716 TFLOP/s); four short sequences 6.8,
-// the time of a launch.  Power is what bounds the long ones: the clock is at 1.9 GHz with the matrix cores busy for 47 % of its cycles and the vector
+// the time of a launch.  Power is what bounds the long ones: the clock is at 1.5 to 1.9 GHz with the matrix cores busy for 47 to 52 % of its cycles and the vector
 // units for 55 %.  Slower or no faster: the next tile's scores between the probabilities (1300), two waves of a SIMD held half a step apart by
 // barriers (1000, and short sequences 30 % slower), tiles of 32 keys with three waves a SIMD (1010, odd lengths 12 % slower).
 #include "lomo_window_common.h"
