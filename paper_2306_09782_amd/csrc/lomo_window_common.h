@@ -118,16 +118,16 @@ struct TileLoad {
             if constexpr (PER == 4)
                 asm volatile("s_mov_b32 m0, %8\n\ts_nop 0\n\t"
                              "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
-                             "buffer_load_dwordx4 %1, %4, %5 offen offset:1024 lds\n\t"
-                             "buffer_load_dwordx4 %2, %4, %6 offen offset:2048 lds\n\t"
-                             "buffer_load_dwordx4 %3, %4, %7 offen offset:3072 lds"
+                             "buffer_load_dwordx4 %1, %4, %5 offen offset:0x400 lds\n\t"
+                             "buffer_load_dwordx4 %2, %4, %6 offen offset:0x800 lds\n\t"
+                             "buffer_load_dwordx4 %3, %4, %7 offen offset:0xc00 lds"
                              ::"v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(srd), "s"(step), "s"(2 * step), "s"(3 * step), "s"(lds) : "memory", "m0");
             else if constexpr (PER == 1)
                 asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(v[0]), "s"(srd), "s"(lds) : "memory", "m0");
             else
                 asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\t"
                              "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
-                             "buffer_load_dwordx4 %1, %2, %3 offen offset:1024 lds"
+                             "buffer_load_dwordx4 %1, %2, %3 offen offset:0x400 lds"
                              ::"v"(v[0]), "v"(v[1]), "s"(srd), "s"(step), "s"(lds) : "memory", "m0");
         } else {      // the descriptor ends behind the last row
             left -= WROWS * wave;
