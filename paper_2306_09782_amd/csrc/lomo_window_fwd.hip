@@ -99,7 +99,8 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void window_attention_forward
         for (int ks = 0; ks < D / 16; ++ks) S = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.rows(32 * h * D, ks), fq[ks], S, 0, 0, 0);
     };
     // From scores to probabilities relative to the running maximum, in fp16.  The maximum moves only where it has grown by more than
-    // SLACK: probabilities stay below 2^SLACK, and most tiles leave sum and output as they are.
+    // SLACK: probabilities stay below 2^SLACK, and most tiles leave sum and output as they are.  Each query moves by its own scores alone,
+    // so that no bit of its result depends on what its neighbours see.
     constexpr float SLACK = 8.f;
     auto probabilities = [&](const floatx16 (&S)[2], uint32_t (&pk)[2][8]) {
         float top = -INFINITY;
@@ -110,7 +111,8 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void window_attention_forward
         const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * C2;
         if (__any(top > m_run + SLACK)) {
-            const float m_new = fmaxf(m_run, top), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+            const bool grown = top > m_run + SLACK;
+            const float m_new = grown ? top : m_run, alpha = grown ? __builtin_amdgcn_exp2f(m_run - top) : 1.f;
 #pragma unroll
             for (int i = 0; i < NC; ++i)
 #pragma unroll
