@@ -158,8 +158,8 @@ constexpr int STAT_BYTES = 2 * 2 * BLK * 4;      // lse and delta of the queries
 template <int D>
 constexpr int KEY_LDS_BYTES = DQ_LDS_BYTES<D> + STAT_BYTES + attn::XCH_BYTES;
 
-// The moving pairs of the kernel that owns keys: q and do of 64 queries of a head, and their lse and delta.  Rows behind the sequence are zeros with
-// an lse of infinity: their probabilities are 0.
+// The moving pairs of the kernel that owns keys: q and do of 64 queries of a head, and their lse and delta.  Rows behind the sequence are zeros; what
+// they give is taken out with what the mask hides, since 0 * inf, for a key that is not finite, is not 0.
 template <int D>
 struct QueryTiles {
     const BwdArgs& a;
@@ -185,7 +185,6 @@ struct QueryTiles {
         if (wave < 2) {
             const float* row = stat0 + (int64_t)tile * (BLK * a.b.h) + n;
             stat = row[(uint32_t)(min(lane, left - 1) * a.b.h)];
-            if (lane >= left) stat = wave == 0 ? INFINITY : 0.f;
         }
     }
     // this wave's share of what fetch() brought; a barrier has to follow
@@ -402,6 +401,7 @@ __global__ __launch_bounds__(512, 2) void window_attention_dkdv_kernel(win::BwdA
     const bool active = kw < s.len && (near == 0 || kw < a.b.sinks);
     const int64_t ld = (int64_t)(a.b.h + 2 * a.b.g) * D;
     const int64_t t = (int64_t)s.start + min(key, s.len - 1);
+    const uint32_t reach_key = min(reach, (uint32_t)max(s.len - key - near, 0));      // no further than the last query
 
     // the walk: (head, tile); this team's steps are `steps` from its `tile` and head `n` on, the other's tile is `other`
     const int per = last - first + 1, total = per * r, more = (total + 1) / 2, fewer = total - more;      // of the first team, of the second
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(512, 2) void window_attention_dkdv_kernel(win::BwdA
     };
     auto own_gradients = [&](int buf, int distance, auto cut, half8 (&f)[2]) {
         half8 fp[2], fd[2];
-        key_gradients<D, decltype(cut)::value>(rd.at(buf * PAIR<D> + 32 * part * D), stats + 2 * buf * BLK + 32 * part, fk, fv, distance, reach, fp, fd);
+        key_gradients<D, decltype(cut)::value>(rd.at(buf * PAIR<D> + 32 * part * D), stats + 2 * buf * BLK + 32 * part, fk, fv, distance, reach_key, fp, fd);
         if (part == 0) xch.put(fd);
         else xch.put(fp);
 #pragma unroll
@@ -446,8 +446,8 @@ __global__ __launch_bounds__(512, 2) void window_attention_dkdv_kernel(win::BwdA
     };
     // where half h of do (for dv) or q (for dk) is
     auto sums_of = [&](int buf, int h) { return rd.at(buf * PAIR<D> + (part == 0 ? TILE<D> : 0) + 32 * h * D); };
-    // the query tiles that are within the bounds for every key of the workgroup
-    const int whole0 = (k0 + BLK - 1 + near + BLK - 1) / BLK, whole1 = near > 0 ? last : (k0 + a.b.window - BLK) / BLK;
+    // the query tiles that are within the bounds for every key of the workgroup, and within the sequence
+    const int whole0 = (k0 + BLK - 1 + near + BLK - 1) / BLK, whole1 = min(near > 0 ? last : (k0 + a.b.window - BLK) / BLK, s.len / BLK - 1);
     auto whole = [&](int x) { return x >= whole0 && x <= whole1; };
     while (it < more) {
         while (it < more && !(it < fewer && whole(tile) && whole(other))) {
