@@ -416,7 +416,8 @@ lomo_status lomo_window_attention_forward(const lomo_half* qkv, lomo_half* o, fl
 
 /* Its gradient: dqkv [T x (n_heads + 2 n_kv_heads) head_dim] out: dq | dk | dv with respect to the rotated q, rotated k and v
  * (lomo_rope_axes with `inverse` on the heads of dq and dk follows).  o, lse: what the forward left; dO [T x n_heads * head_dim].
- * dk and dv of a key head are sums over its query heads, in fp32.  P and dS pass through fp16 before the products that consume them.
+ * dk and dv of a key head are sums over its query heads, in fp32.  P and dS pass through fp16 before the products that consume them, dS at a
+ * power of two that follows its row (the query of dq, the key of dk): no size of dO loses bits there or overflows.
  * Rows that belong to no sequence are left as they are.  ws: device workspace, 16-byte aligned, of at least
  * lomo_window_attention_workspace_bytes(...) bytes (do . o of every row and head, and partial sums of the sinks' gradients, whose queries
  * are the whole sequence); no need to clear it; calls that overlap in time need one each.  dqkv may not alias the inputs.  Deterministic (no

@@ -12,7 +12,8 @@
 // and rounds.  All recompute S, P, dP, dS in blocks of 32 x 32 per wave with the wave's own rows along the lanes.
 //
 // fp32 accumulation on the matrix cores.  P and dS pass through fp16 before the products that consume them; P is held times 2^15 there,
-// so that the probabilities of a long window (2^-14 and less) keep all their bits.  dq, dk, dv are rounded once.  Tiles that a mask cuts are
+// so that the probabilities of a long window (2^-14 and less) keep all their bits, and dS times a power of two of its own row (below), so that
+// gradients of any size do.  dq, dk, dv are rounded once.  Tiles that a mask cuts are
 // made finite first, so that a pair which the mask hides adds nothing; a query that sees a key which is not finite has NaN in its gradient.
 //
 // Measured, us: 16384 tokens, 32 / 8 heads of 128, window 2048, 4 sinks 2190 (dq 800, dk and dv 1390; 588 TFLOP/s of the five products, 820 of
@@ -35,6 +36,45 @@ constexpr int FAR_ROWS = 512;
 constexpr float P_SCALE = 32768.f, P_LOG2 = 15.f;
 template <int D>
 constexpr float DS_SCALE = SCALE<D> / P_SCALE;      // of dP - delta where it meets P times P_SCALE
+
+// dS passes through fp16 times 2^e, with an e for each query of dq and each key of dk.  It begins high and falls where a block has a dS beyond
+// DS_TOP, to where the largest is 2^DS_TARGET .. 2^(DS_TARGET + 1); the sums fall with it.  So what is within 2^-21 of the largest that the row has met keeps all
+// its bits, whatever the size of dO and v, and nothing overflows that the result holds.  A row's e follows from what the row sees alone.
+constexpr int DS_FIRST = 60, DS_LAST = -60, DS_TARGET = 7;
+constexpr float DS_TOP = 32768.f;
+__device__ __forceinline__ float power_of_2(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }
+// lower(n): e has fallen by n (0 for rows that stay).  A dS that is infinite before it is scaled stays so.
+template <typename F>
+__device__ __forceinline__ void keep_in_range(floatx16& dS, int& exponent, F&& lower) {
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(dS[e]));
+    if (__any(top > DS_TOP)) {
+        const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+        const int n = top > DS_TOP && top < INFINITY ? min((int)(__float_as_uint(top) >> 23) - 127 - DS_TARGET, exponent - DS_LAST) : 0;
+        const float f = power_of_2(-n);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dS[e] *= f;
+        exponent -= n;
+        lower(n);
+    }
+}
+template <int N>
+__device__ __forceinline__ void multiply_all(floatx16 (&x)[N], float f) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[i][e] *= f;
+}
+__device__ __forceinline__ void fragments(const floatx16& x, half8 (&f)[2]) {
+    uint32_t pk[8];
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) pk[e >> 1] = pack2(x[e], x[e + 1]);
+    __builtin_amdgcn_sched_barrier(0);
+    f[0] = fragment_of(pk, 0);
+    f[1] = fragment_of(pk, 1);
+}
 template <int D>
 constexpr float SCALE_LOG2 = D == 128 ? 3.5f : 3.f;      // log2(sqrt(D))
 
@@ -78,11 +118,11 @@ __device__ __forceinline__ float row_product(const half8 (&fo)[D / 16], const ha
     return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
 }
 
-// S and dP of a block: rows 0 .. 31 of the pair's tiles against the wave's fragments.
+// S and, added to P, dP of a block: rows 0 .. 31 of the pair's tiles against the wave's fragments.
 template <int D>
 __device__ __forceinline__ void products(const TileRead<D>& r0, const half8 (&fx)[D / 16], const half8 (&fy)[D / 16], floatx16& S, floatx16& P) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) S[e] = P[e] = 0.f;
+    for (int e = 0; e < 16; ++e) S[e] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
         S = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.rows(0, ks), fx[ks], S, 0, 0, 0);
@@ -110,23 +150,32 @@ __device__ __forceinline__ void clear(floatx16 (&x)[N]) {
         for (int e = 0; e < 16; ++e) x[i][e] = 0.f;
 }
 
-// P (times P_SCALE) and dS of a block as fragments, for a wave that owns keys: queries qb .. qb + 31 (rows 0 .. 31 of the pair q, do;
-// stats: their lse log2(e) - 15 and, BLK further on, delta DS_SCALE) against the lane's key.  CUT: without the pairs whose distance is not one of the
+// P (times P_SCALE) and dS (times `scale` / DS_SCALE) of a block, for a wave that owns keys: queries qb .. qb + 31 (rows 0 .. 31 of the pair q, do;
+// stats: their lse log2(e) - 15 and, BLK further on, -delta) against the lane's key.  CUT: without the pairs whose distance is not one of the
 // `reach` from `near` on.
 template <int D, bool CUT>
 __device__ __forceinline__ void key_gradients(const TileRead<D>& r0, const float* stats, const half8 (&fk)[D / 16], const half8 (&fv)[D / 16],
-                                              int distance, uint32_t reach, half8 (&fp)[2], half8 (&fd)[2]) {
+                                              int distance, uint32_t reach, float scale, half8 (&fp)[2], floatx16& dS) {
     constexpr float C2 = SCALE<D> * LOG2E;
     const int lh = (threadIdx.x & 63) >> 5;
     floatx16 S, P;
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+        const float4 d4 = *reinterpret_cast<const float4*>(stats + BLK + 8 * g4 + 4 * lh);
+        P[4 * g4] = d4.x;
+        P[4 * g4 + 1] = d4.y;
+        P[4 * g4 + 2] = d4.z;
+        P[4 * g4 + 3] = d4.w;
+    }
+    __builtin_amdgcn_sched_barrier(0);
     products<D>(r0, fk, fv, S, P);
 #pragma unroll
     for (int g4 = 0; g4 < 4; ++g4) {
-        const float4 l4 = *reinterpret_cast<const float4*>(stats + 8 * g4 + 4 * lh), d4 = *reinterpret_cast<const float4*>(stats + BLK + 8 * g4 + 4 * lh);
-        const float lq[4] = {l4.x, l4.y, l4.z, l4.w}, dq[4] = {d4.x, d4.y, d4.z, d4.w};
+        const float4 l4 = *reinterpret_cast<const float4*>(stats + 8 * g4 + 4 * lh);
+        const float lq[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            float p = __builtin_amdgcn_exp2f(fmaf(C2, S[4 * g4 + e], -lq[e])), d = fmaf(DS_SCALE<D>, P[4 * g4 + e], -dq[e]);
+            float p = __builtin_amdgcn_exp2f(fmaf(C2, S[4 * g4 + e], -lq[e])), d = P[4 * g4 + e] * scale;
             if constexpr (CUT) {
                 p = not_finite(d) ? NAN : p;
                 asm volatile("" : "+v"(p), "+v"(d));      // selects, no branches
@@ -135,28 +184,17 @@ __device__ __forceinline__ void key_gradients(const TileRead<D>& r0, const float
                 d = hidden ? 0.f : d;
             }
             S[4 * g4 + e] = p;
-            P[4 * g4 + e] = d;
+            dS[4 * g4 + e] = p * d;
         }
     }
-    uint32_t pp[8], pd[8];
-#pragma unroll
-    for (int e = 0; e < 16; e += 2) {
-        pp[e >> 1] = pack2(S[e], S[e + 1]);
-        pd[e >> 1] = pack2(S[e] * P[e], S[e + 1] * P[e + 1]);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-        fp[ks] = fragment_of(pp, ks);
-        fd[ks] = fragment_of(pd, ks);
-    }
+    fragments(S, fp);
 }
 
 template <int D>
 constexpr int DQ_LDS_BYTES = 2 * PAIR<D> * 2;
 constexpr int STAT_BYTES = 2 * 2 * BLK * 4;      // lse and delta of the queries of two pairs
 template <int D>
-constexpr int KEY_LDS_BYTES = DQ_LDS_BYTES<D> + STAT_BYTES + attn::XCH_BYTES;
+constexpr int KEY_LDS_BYTES = DQ_LDS_BYTES<D> + STAT_BYTES + attn::XCH_BYTES + 4 * 64 * 4;      // the last: exponents that go with the exchange
 
 // The moving pairs of the kernel that owns keys: q and do of 64 queries of a head, and their lse and delta.  Rows behind the sequence are zeros; what
 // they give is taken out with what the mask hides, since 0 * inf, for a key that is not finite, is not 0.
@@ -189,7 +227,7 @@ struct QueryTiles {
     }
     // this wave's share of what fetch() brought; a barrier has to follow
     __device__ __forceinline__ void keep_stats(int buf) const {
-        if (wave < 2) stats[(2 * buf + wave) * BLK + lane] = wave == 0 ? fmaf(stat, LOG2E, -P_LOG2) : stat * DS_SCALE<D>;
+        if (wave < 2) stats[(2 * buf + wave) * BLK + lane] = wave == 0 ? fmaf(stat, LOG2E, -P_LOG2) : -stat;
     }
 };
 
@@ -246,7 +284,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
         load_fragments<D>(fd, a.dO + t * ldo + (int64_t)n * D);
         half8 fo[D / 16];
         load_fragments<D>(fo, a.o + t * ldo + (int64_t)n * D);
-        lq = fmaf(a.lse[t * a.b.h + n], LOG2E, SCALE_LOG2<D>);      // so that P comes with the scale of dS
+        lq = fmaf(a.lse[t * a.b.h + n], LOG2E, SCALE_LOG2<D> - DS_FIRST);      // so that P comes with the scale of dS
         delta = row_product<D>(fo, fd);
         if (lh == 0 && query < s.len) a.delta[t * a.b.h + n] = delta;
     }
@@ -255,13 +293,15 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
     asm volatile("" : "+v"(lq));
     floatx16 acc[D / 32];
     clear(acc);
+    int exponent = DS_FIRST;
 
     // dS of keys k0 .. k0 + 31 as fragments.  Bits of `rows`: keys that are not finite; a query that sees one has an lse and a delta that are not,
     // unless its score is -inf: then P is 0 and dS times the key is NaN in its infinite columns.
     auto gradients = [&](const TileRead<D>& r0, int k0, auto cut, uint32_t rows, half8 (&f)[2]) {
         floatx16 S, P;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) P[e] = 0.f;
         products<D>(r0, fq, fd, S, P);
-        uint32_t pk[8];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             S[e] = __builtin_amdgcn_exp2f(fmaf(C2, S[e], -lq));
@@ -281,10 +321,12 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
             for (int e = 0; e < 16; ++e) S[e] = own >> (8 * (e >> 2) + (e & 3)) & 1 ? 0.f : S[e];
         }
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) pk[e >> 1] = pack2(S[e] * P[e], S[e + 1] * P[e + 1]);
-        __builtin_amdgcn_sched_barrier(0);
-        f[0] = fragment_of(pk, 0);
-        f[1] = fragment_of(pk, 1);
+        for (int e = 0; e < 16; ++e) S[e] *= P[e];
+        keep_in_range(S, exponent, [&](int n) {
+            lq += (float)n;
+            multiply_all(acc, power_of_2(-n));
+        });
+        fragments(S, f);
     };
 
     int it = 0;
@@ -340,6 +382,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
             }
         }
     }
+    multiply_all(acc, power_of_2(-exponent));
     if (active) store_rows(acc, query < s.len ? a.dqkv + t * ld + (int64_t)n * D : nullptr);
 }
 
@@ -361,6 +404,7 @@ __global__ __launch_bounds__(512, 2) void window_attention_dkdv_kernel(win::BwdA
     uint16_t* tiles_at = own_lds + STAT_BYTES / 2;
     const uint32_t lds0 = (uint32_t)(uintptr_t)tiles_at;
     const attn::Exchange xch(tiles_at + 2 * PAIR<D>, wave);
+    int* exponents = reinterpret_cast<int*>(tiles_at + 2 * PAIR<D> + attn::XCH_BYTES / 2) + lane;
 
     const int r = a.b.h / a.b.g;
     int seq, kv, k0, near, first, last;      // keys from k0 on; query tiles; the distance of the nearest query
@@ -419,6 +463,8 @@ __global__ __launch_bounds__(512, 2) void window_attention_dkdv_kernel(win::BwdA
     arrived<D>(fv);
     floatx16 acc[D / 32];      // dv or dk
     clear(acc);
+    int exponent = DS_FIRST;      // of this wave's dS, and of the sums for dk
+    float scale = power_of_2(DS_FIRST) * DS_SCALE<D>;
     const TileRead<D> rd(lds0);
 
     int it = 0;
@@ -436,13 +482,39 @@ __global__ __launch_bounds__(512, 2) void window_attention_dkdv_kernel(win::BwdA
         if (it < steps) tiles.fetch(tile, n, buf ^ 1);      // in flight while this pair is multiplied
         return buf;
     };
+    auto lower = [&](int n) {
+        const float f = power_of_2(-n);
+        scale *= f;
+        if (part == 1) multiply_all(acc, f);
+    };
     auto own_gradients = [&](int buf, int distance, auto cut, half8 (&f)[2]) {
         half8 fp[2], fd[2];
-        key_gradients<D, decltype(cut)::value>(rd.at(buf * PAIR<D> + 32 * part * D), stats + 2 * buf * BLK + 32 * part, fk, fv, distance, reach_key, fp, fd);
+        floatx16 dS;
+        key_gradients<D, decltype(cut)::value>(rd.at(buf * PAIR<D> + 32 * part * D), stats + 2 * buf * BLK + 32 * part, fk, fv, distance, reach_key, scale, fp, dS);
+        keep_in_range(dS, exponent, lower);
+        fragments(dS, fd);
+        exponents[64 * wave] = exponent;
         if (part == 0) xch.put(fd);
         else xch.put(fp);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) f[ks] = part == 0 ? fp[ks] : fd[ks];
+    };
+    // the partner's half; both go on with the lower exponent of the two
+    auto others_gradients = [&](half8 (&f)[2]) {
+        xch.get(f);
+        const int other_exponent = exponents[64 * (wave ^ 2)];
+        if (__any(other_exponent != exponent)) {
+            if (part == 1) {
+                const float down = power_of_2(-max(other_exponent - exponent, 0));
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[ks][e] = (_Float16)((float)f[ks][e] * down);
+            }
+            const int n = max(exponent - other_exponent, 0);
+            exponent -= n;
+            lower(n);
+        }
     };
     // where half h of do (for dv) or q (for dk) is
     auto sums_of = [&](int buf, int h) { return rd.at(buf * PAIR<D> + (part == 0 ? TILE<D> : 0) + 32 * h * D); };
@@ -466,7 +538,7 @@ __global__ __launch_bounds__(512, 2) void window_attention_dkdv_kernel(win::BwdA
             }
             attn::meet();
             if (some(1 - part)) {
-                xch.get(f);
+                others_gradients(f);
                 multiply<D>(sums_of(buf, 1 - part), 0, f, acc);
             }
         }
@@ -479,10 +551,11 @@ __global__ __launch_bounds__(512, 2) void window_attention_dkdv_kernel(win::BwdA
             }
             attn::meet();
             if (!active) continue;
-            xch.get(f);
+            others_gradients(f);
             multiply<D>(sums_of(buf, 1 - part), 0, f, acc);
         }
     }
+    multiply_all(acc, part == 0 ? 1.f / P_SCALE : power_of_2(-exponent));
     // the second team's sums to the first
     float* sums = reinterpret_cast<float*>(smem) + wave * (D / 2 * 64) + lane;      // as much as two pairs of tiles
     __syncthreads();
@@ -498,12 +571,6 @@ __global__ __launch_bounds__(512, 2) void window_attention_dkdv_kernel(win::BwdA
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][e] += sums[(16 * i + e) * 64];
-    if (part == 0) {
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][e] *= 1.f / P_SCALE;
-    }
     const bool own = key < s.len, sink = own && key < a.b.sinks && slot != nullptr;
     if (near == 0) store_rows(acc, own && !sink ? a.dqkv + t * ld + (int64_t)(a.b.h + (1 - part) * a.b.g + kv) * D : nullptr);
     if (sink) {
