@@ -435,7 +435,7 @@ size_t lomo_window_attention_workspace_bytes(int64_t T, int64_t B, int64_t n_hea
  *   loss = (1 - w) (lse(z) - z[target]) + w tau^2 sum_k p_k (log p_k - log q[id_k]),
  *   dlogits_j = grad_scale * ((1 - w) (softmax(z)_j - [j = target]) + w tau (q_j - sum of p_k with id_k = j)).
  * An id outside [0, V) or a teacher logit of -inf is not listed; an id listed twice has both its shares; a token with nothing listed
- * has the first term alone.  targets [T] int32: a target outside [0, V) leaves its token out (loss 0, zero gradient row), also where
+ * has the first term alone, and so has every token where w = 0, whatever the teacher's logits hold.  targets [T] int32: a target outside [0, V) leaves its token out (loss 0, zero gradient row), also where
  * w = 1.  1 <= K <= 1024, V % 8 == 0, T < 2^22, 2^-10 <= tau <= 2^10.  loss [T] fp32.  dlogits may be the logits buffer itself.  Deterministic. */
 lomo_status lomo_distill(const lomo_half* logits, const int32_t* teacher_ids, const lomo_half* teacher_logits, const int32_t* targets,
                          float grad_scale, float temperature, float soft_weight, float* loss, lomo_half* dlogits,

@@ -174,7 +174,7 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
     all.soft = wave_sum(all.soft);
     if constexpr (BOTH) all.hard = wave_sum(all.hard);
     const float kh = all.kh, ks = all.ks, soft = all.soft, hard = BOTH ? all.hard : all.soft;
-    const bool taught = top > -INFINITY;      // otherwise nothing is listed and the soft term is left out
+    const bool taught = a.w > 0.f && top > -INFINITY;      // otherwise it has no weight, or nothing is listed: the soft term is left out
     const float w = taught ? a.w : 0.f, as = scale * w * a.tau / soft, ah = scale * (1.f - a.w) / hard;
     const float alone = as + ah;              // of the one exponential
     {
