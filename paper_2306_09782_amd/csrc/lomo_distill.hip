@@ -87,7 +87,7 @@ struct Sums {
 template <int NT, int CH, bool BOTH>
 __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) {
     constexpr int WAVES = NT / 64;
-    extern __shared__ float lds[];      // p, z and id of the listed columns and of the target (the last)
+    extern __shared__ float lds[];      // teacher's logit and then p, z and id of the listed columns and of the target (the last)
     __shared__ float red[5][WAVES];
     float* p = lds;
     float* zk = lds + a.K + 1;
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
     float top = -INFINITY;
     auto keep = [&](int k, int i, float z, float l) {
         const bool in = i >= 0 && i < a.V;
-        p[k] = k < a.K && in ? l / a.tau : -INFINITY;
+        p[k] = k < a.K && in ? l : -INFINITY;
         zk[k] = z;
         id[k] = in ? i : -1;
         top = fmaxf(top, p[k]);
@@ -179,7 +179,11 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
     const float alone = as + ah;              // of the one exponential
     {
         float sum = 0.f;
-        for (int k = threadIdx.x; k < a.K; k += NT) sum += taught ? expf(p[k] - top) : 0.f;
+        for (int k = threadIdx.x; k < a.K; k += NT) {
+            const float x = (p[k] - top) / a.tau;      // of the difference, which is exact or nearly so: the logits themselves may be long at a small tau
+            p[k] = x;
+            sum += taught ? expf(x) : 0.f;
+        }
         sum = wave_sum(sum);
         if (lane == 0) red[4][wave] = sum;
     }
@@ -195,10 +199,10 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
         return o;
     };
     __syncthreads();
-    const float teacher_lse = top + logf(wave_sum(has ? red[4][lane] : 0.f)), log_soft = __builtin_amdgcn_logf(soft);
+    const float log_sum = logf(wave_sum(has ? red[4][lane] : 0.f)), log_soft = __builtin_amdgcn_logf(soft);
     float divergence = 0.f;
     for (int k = threadIdx.x; k < a.K; k += NT) {
-        const float log_p = p[k] - teacher_lse, pk = taught ? expf(log_p) : 0.f;
+        const float log_p = p[k] - log_sum, pk = taught ? expf(log_p) : 0.f;
         if (pk != 0.f) divergence += pk * (log_p - LN2 * (fmaf(zk[k], cs, -ks) - log_soft));
         p[k] = pk;
     }

@@ -45,3 +45,41 @@ def test_a_teacher_without_weight_does_not_matter(L, tau):
     teacher[3] = np.nan
     got = run(L, z, ids, teacher, targets, 16.0, tau, 0.0)
     assert np.array_equal(got[0], clean[0]) and np.array_equal(got[1], clean[1]) and np.isfinite(clean[1]).all()
+
+
+def definition(z, ids, teacher, target, tau, w):
+    """One token: loss, gradient, and the size of what their errors are relative to."""
+    z, t = z.astype(np.float64), teacher.astype(np.float64)
+    log_p = (t - t.max()) / tau - np.log(np.exp((t - t.max()) / tau).sum())
+    log_q = (z - z.max()) / tau - np.log(np.exp((z - z.max()) / tau).sum())
+    log_1 = (z - z.max()) - np.log(np.exp(z - z.max()).sum())
+    p = np.exp(log_p)
+    loss = -(1 - w) * log_1[target] + w * tau ** 2 * (p * (log_p - log_q[ids])).sum()
+    size = (1 - w) * (1 - log_1[target]) + w * tau ** 2 * (1 + (p * (abs(log_p) + abs(log_q[ids]))).sum())
+    grad = (1 - w) * np.exp(log_1) + w * tau * np.exp(log_q)
+    grad[target] -= 1 - w
+    np.subtract.at(grad, ids, w * tau * p)
+    return loss, grad, size
+
+
+# fp32 arguments of exponentials of up to 64 (what is below adds nothing), 2^-24 of each, and sums of 2^10 terms: 2^-17 covers them
+NEAR = 2.0 ** -17
+
+
+@pytest.mark.parametrize("tau,shift,step", [(2.0 ** -10, 60000.0, 32.0), (2.0 ** -6, 20.0, 2.0 ** -6), (2.0 ** -8, 1000.0, 1.0), (2.0, 30000.0, 16.0),
+                                            (2.0 ** 10, 30000.0, 16.0)])
+@pytest.mark.parametrize("w", [0.6, 1.0])
+def test_differences_of_large_teacher_logits(L, tau, shift, step, w):
+    T, V, K = 8, 64, 9
+    rng = np.random.default_rng(3)
+    z = rng.standard_normal((T, V)).astype(np.float16) * np.float16(min(tau, 1.0))
+    ids = np.stack([rng.permutation(V)[:K] for _ in range(T)])
+    teacher = (shift + step * rng.integers(-3, 1, (T, K))).astype(np.float16)
+    teacher[0] = teacher[0, 0]                       # all alike
+    targets, scale = ids[:, 1], 8.0 / min(tau, 1.0)
+    loss, dz = run(L, z, ids, teacher, targets, scale, tau, w)
+    for t in range(T):
+        want, grad, size = definition(z[t], ids[t], teacher[t], targets[t], tau, w)
+        grad, most = scale * grad, scale * ((1 - w) + w * tau)
+        assert abs(loss[t] - want) <= NEAR * size, (t, loss[t], want)
+        assert (np.abs(dz[t] - grad) <= S.H16 * np.abs(grad) + NEAR * most + S.TINY16).all(), t
