@@ -225,7 +225,7 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
     const float sum = wave_sum(has ? red[3][lane] : 0.f);
     if (threadIdx.x == 0) {
         float l = w > 0.f ? w * a.tau * a.tau * sum : 0.f;
-        if (a.w != 1.f) l += (1.f - a.w) * (LN2 * (kh + __builtin_amdgcn_logf(hard)) - zk[a.K]);
+        if (a.w != 1.f) l += (1.f - a.w) * LN2 * (__builtin_amdgcn_logf(hard) - fmaf(zk[a.K], ch, -kh));      // no difference of long numbers
         a.loss[t] = l;
     }
     for (int k = threadIdx.x; k <= a.K; k += NT) {

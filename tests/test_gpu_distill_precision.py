@@ -83,3 +83,18 @@ def test_differences_of_large_teacher_logits(L, tau, shift, step, w):
         grad, most = scale * grad, scale * ((1 - w) + w * tau)
         assert abs(loss[t] - want) <= NEAR * size, (t, loss[t], want)
         assert (np.abs(dz[t] - grad) <= S.H16 * np.abs(grad) + NEAR * most + S.TINY16).all(), t
+
+
+@pytest.mark.parametrize("shift", [0.0, 1000.0, 30000.0, 60000.0, -60000.0])
+@pytest.mark.parametrize("w,tau", [(0.0, 2.0), (0.5, 1.0), (0.5, 4.0)])
+def test_loss_of_large_logits(L, shift, w, tau):
+    T, V, K = 6, 1000, 5
+    rng = np.random.default_rng(4)
+    z = (shift + 2 * rng.standard_normal((T, V))).astype(np.float16)
+    ids = np.stack([rng.permutation(V)[:K] for _ in range(T)])
+    teacher, targets = rng.standard_normal((T, K)).astype(np.float16), ids[:, 2]
+    loss, dz = run(L, z, ids, teacher, targets, 64.0, tau, w)
+    for t in range(T):
+        want, grad, size = definition(z[t], ids[t], teacher[t], targets[t], tau, w)
+        assert abs(loss[t] - want) <= NEAR * size, (t, loss[t], want)
+        assert (np.abs(dz[t] - 64 * grad) <= (S.H16 + NEAR) * np.abs(64 * grad) + 64 * NEAR * tau + S.TINY16).all(), t
