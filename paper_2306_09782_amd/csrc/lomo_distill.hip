@@ -32,7 +32,7 @@ struct Distill {
     uint16_t* dz;
     int64_t V;
     int K;
-    float scale, tau, w;
+    float scale, tau, inv_tau, w;
 };
 
 __device__ __forceinline__ float wave_max(float v) {
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
     {
         float sum = 0.f;
         for (int k = threadIdx.x; k < a.K; k += NT) {
-            const float x = (p[k] - top) / a.tau;      // of the difference, which is exact or nearly so: the logits themselves may be long at a small tau
+            const float x = (p[k] - top) * a.inv_tau;      // of the difference, which is exact or nearly so: the logits themselves may be long at a small tau
             p[k] = x;
             sum += taught ? expf(x) : 0.f;
         }
@@ -257,7 +257,7 @@ hipError_t launch(const Distill& a, int64_t T, hipStream_t st) {
 hipError_t launch_distill(const uint16_t* z, const int32_t* ids, const uint16_t* teacher, const int32_t* target, float scale,
                           const float* scale_dev, float tau, float w, float* loss, uint16_t* dz, int64_t T, int64_t V, int64_t K,
                           hipStream_t st) {
-    const Distill a = {z, ids, teacher, target, scale_dev, loss, dz, V, (int)K, scale, tau, w};
+    const Distill a = {z, ids, teacher, target, scale_dev, loss, dz, V, (int)K, scale, tau, 1.f / tau, w};
     const int64_t chunks = V / 8;
     // The smallest workgroup whose registers hold the row, so that several share a CU and one computes while another reads.  us, with the next larger instead:
     // 8192 x 8000 62 / 88 (256 and 512 threads), 4096 x 32008 108 / 161 (512 threads of eight chunks, 1024 of four), 2048 x 60000 108 / 152 (eight
