@@ -142,7 +142,7 @@ __global__ __launch_bounds__(NT, CH > 8 ? 4 : 8) void distill_kernel(Distill a) 
         p[k] = k < a.K && in ? l : -INFINITY;
         zk[k] = z;
         id[k] = in ? i : -1;
-        top = fmaxf(top, p[k]);
+        top = fmaxf(top, p[k] != p[k] ? INFINITY : p[k]);      // a maximum passes over NaN, which is listed all the same
     };
     if ((int)threadIdx.x <= a.K) keep(threadIdx.x, own, own_z, own_logit);
     for (int k = threadIdx.x + NT; k <= a.K; k += NT) {

@@ -98,3 +98,17 @@ def test_loss_of_large_logits(L, shift, w, tau):
         want, grad, size = definition(z[t], ids[t], teacher[t], targets[t], tau, w)
         assert abs(loss[t] - want) <= NEAR * size, (t, loss[t], want)
         assert (np.abs(dz[t] - 64 * grad) <= (S.H16 + NEAR) * np.abs(64 * grad) + 64 * NEAR * tau + S.TINY16).all(), t
+
+
+@pytest.mark.parametrize("w", [0.5, 1.0])
+@pytest.mark.parametrize("K", [1, 4, 700])
+def test_a_teacher_of_nothing_but_nan_is_seen(L, w, K):
+    z, ids, teacher, targets = rows(6, 4, 520, K)
+    clean = run(L, z, ids, teacher, targets, 16.0, 2.0, w)
+    teacher[1], teacher[2, 1:] = np.nan, -np.inf      # all NaN; one listed
+    teacher[3, -1] = np.nan
+    got = run(L, z, ids, teacher, targets, 16.0, 2.0, w)
+    assert got[0][0] == clean[0][0] and np.array_equal(got[1][0], clean[1][0])
+    for t in (1, 3):
+        assert not np.isfinite(got[0][t]) and not np.isfinite(got[1][t]).all(), t
+    assert np.isfinite(got[0][2]) and np.isfinite(got[1][2]).all()
