@@ -429,6 +429,10 @@ lomo_status lomo_window_attention_backward(const lomo_half* qkv, const lomo_half
 /* 0 for T == 0, B == 0 or sizes that the calls refuse (host function). */
 size_t lomo_window_attention_workspace_bytes(int64_t T, int64_t B, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, int64_t sinks);
 
+/* Zeros in the rows of x [T x width] that belong to no sequence (before seq_offsets[0], from seq_offsets[B] on): what the two calls above leave as it
+ * was, where products over all T rows follow.  The offsets are read on the device, so that a captured call takes other batches.  width % 8 == 0. */
+lomo_status lomo_clear_padding(lomo_half* x, const int32_t* seq_offsets, int64_t T, int64_t B, int64_t width, void* stream);
+
 /* Token losses and their scaled gradient for a student with logits z [T x V] whose teacher is known by K top logits a token
  * (teacher_ids int32 [T x K], teacher_logits [T x K]), at a temperature tau, with weight w = soft_weight in [0, 1]:
  *   p = softmax(teacher_logits / tau) over the listed ones,  q = softmax(z / tau),

@@ -18,7 +18,7 @@ from .binding import (LomoError, library_path, load_library, lomo_version, lomo_
                       lomo_linear_forward, lomo_rmsnorm_forward, lomo_swiglu_forward, lomo_rope_forward,
                       lomo_attention_forward, lomo_cross_entropy, lomo_embedding_forward, lomo_linear_forward_residual,
                       lomo_rope_axes, lomo_window_attention_forward, lomo_window_attention_backward,
-                      lomo_window_attention_workspace_bytes, lomo_distill, lomo_distill_mean,
+                      lomo_window_attention_workspace_bytes, lomo_clear_padding, lomo_distill, lomo_distill_mean,
                       lomo_cross_entropy_mean, lomo_vector_update_static, VECTOR_STATIC_BYTES, lomo_probe_mfma, lomo_probe_copy, PROBE_OPERAND_BYTES, on_stream,
                       EXPORTED_SYMBOLS)
 

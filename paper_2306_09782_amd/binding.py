@@ -26,7 +26,7 @@ EXPORTED_SYMBOLS = (
     "lomo_probe_mfma", "lomo_probe_copy", "lomo_vector_update_static", "lomo_contraction_tiles",
     "lomo_contraction_plan",
     "lomo_rope_axes", "lomo_window_attention_forward", "lomo_window_attention_backward", "lomo_window_attention_workspace_bytes",
-    "lomo_distill", "lomo_distill_mean",
+    "lomo_clear_padding", "lomo_distill", "lomo_distill_mean",
 )
 
 
@@ -112,6 +112,7 @@ def load_library():
         "lomo_window_attention_forward": (c_int, [P, P, P, P, I64, I64, I64, I64, I64, I64, I64, P]),
         "lomo_window_attention_backward": (c_int, [P, P, P, P, P, P, I64, I64, I64, I64, I64, I64, I64, P, c_size_t, P]),
         "lomo_window_attention_workspace_bytes": (c_size_t, [I64, I64, I64, I64, I64, I64]),
+        "lomo_clear_padding": (c_int, [P, P, I64, I64, I64, P]),
         "lomo_distill": (c_int, [P, P, P, P, c_float, c_float, c_float, P, P, I64, I64, I64, P]),
         "lomo_distill_mean": (c_int, [P, P, P, P, c_double, c_float, c_float, P, P, P, I64, I64, I64, P]),
         "lomo_timing_enable": (c_int, [c_int]),
@@ -503,6 +504,18 @@ def lomo_window_attention_backward(qkv, o, dO, lse, dqkv, seq_offsets, n_heads, 
     _check(load_library().lomo_window_attention_backward(qkv.data_ptr(), o.data_ptr(), dO.data_ptr(), lse.data_ptr(), dqkv.data_ptr(),
                                                          seq_offsets.data_ptr(), T, B, n_heads, n_kv_heads, d, window, sinks, ws.data_ptr(),
                                                          _nbytes(ws), _raw_stream(stream)))
+
+
+def lomo_clear_padding(x, seq_offsets, stream=None):
+    """Zeros in the rows of x [rows x width] that belong to no sequence."""
+    torch = _torch()
+    device = _device(x, "x")
+    if x.dim() != 2 or seq_offsets.numel() < 1:
+        raise LomoError(f"x {tuple(x.shape)} with {seq_offsets.numel()} offsets, want [rows x width] and [sequences + 1]")
+    _expect(x, torch.float16, x.shape, device, "x")
+    _expect(seq_offsets, torch.int32, (seq_offsets.numel(),), device, "seq_offsets")
+    _check(load_library().lomo_clear_padding(x.data_ptr(), seq_offsets.data_ptr(), x.shape[0], seq_offsets.numel() - 1, x.shape[1],
+                                             _raw_stream(stream)))
 
 
 def _distill_sizes(logits, teacher_ids, teacher_logits, targets, loss, dlogits):

@@ -165,8 +165,8 @@ class PackedAttention:
 
     set_batch(lengths, positions) before a step, on the step's stream: lengths on the host, at most max_sequences of them, their sum at
     most T; positions int32 [axes x T] (None: each token's place in its sequence, on every axis).  Rows behind the last sequence are
-    padding: their targets have to be outside the vocabulary, then they add nothing to any gradient.  A captured step takes further
-    batches with as many tokens as the one that it was captured with."""
+    padding: their targets have to be outside the vocabulary, then they add nothing to any gradient.  The kernels read all of it on the
+    device, so that a captured step takes any further batch."""
 
     def __init__(self, device, T: int, n_heads: int, n_kv_heads: int, head_dim: int, window: int = None, sinks: int = 0,
                  max_sequences: int = 64, pair_axis=None):
@@ -208,21 +208,15 @@ class PackedAttention:
         B.lomo_rope_axes(qkv, qkv, rope_cos, rope_sin, self.positions, self.pair_axis, self.n_heads + self.n_kv_heads, self.head_dim,
                          stream=stream)
         B.lomo_window_attention_forward(qkv, o, lse, self.offsets, self.n_heads, self.n_kv_heads, self.window, self.sinks, stream)
-        self._clear_padding(o, stream)
+        B.lomo_clear_padding(o, self.offsets, stream)       # the attention leaves rows of no sequence as they are; the products that follow take them all
 
     def backward(self, qkv, o, dO, lse, rope_cos, rope_sin, dqkv, stream=None) -> None:
         """dqkv: the gradient of the projection's output."""
         B.lomo_window_attention_backward(qkv, o, dO, lse, dqkv, self.offsets, self.n_heads, self.n_kv_heads, self.window, self.sinks,
                                          self.ws, stream)
-        self._clear_padding(dqkv, stream)
+        B.lomo_clear_padding(dqkv, self.offsets, stream)
         B.lomo_rope_axes(dqkv, dqkv, rope_cos, rope_sin, self.positions, self.pair_axis, self.n_heads + self.n_kv_heads, self.head_dim,
                          inverse=True, stream=stream)
-
-    def _clear_padding(self, x, stream):
-        """The kernels leave rows of no sequence as they are; the products that follow take them all."""
-        if self.rows < self.T:
-            with B.on_stream(stream):
-                x[self.rows:].zero_()
 
 
 class LomoAttentionBlock:

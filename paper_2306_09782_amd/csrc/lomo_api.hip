@@ -750,6 +750,16 @@ lomo_status lomo_window_attention_backward(const lomo_half* qkv, const lomo_half
                                                      window < T ? window : T, sinks, ws, st));
 }
 
+lomo_status lomo_clear_padding(lomo_half* x, const int32_t* seq_offsets, int64_t T, int64_t B, int64_t width, void* stream) {
+    if (T < 0 || B < 0 || width < 0 || (width & 7) || T > 0x7fffffff || width > 0x7fffffff) return LOMO_ERR_SHAPE;
+    if (T == 0 || width == 0) return LOMO_OK;
+    if (!x || !seq_offsets) return LOMO_ERR_NULL;
+    if (misaligned(x) || misaligned4(seq_offsets)) return LOMO_ERR_ALIGN;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ScopedTiming timing(LOMO_KERNEL_CHAIN, st);
+    return from_hip(launch_clear_padding(x, seq_offsets, T, B, width, st));
+}
+
 }  // extern "C"
 
 // What lomo_distill and lomo_distill_mean ask of what they share.

