@@ -164,7 +164,7 @@ class PackedAttention:
     [positions x head_dim / 2].  window=None: no limit.  pair_axis: the axis of each of the head_dim / 2 pairs (None: one axis).
 
     set_batch(lengths, positions) before a step, on the step's stream: lengths on the host, at most max_sequences of them, their sum at
-    most T; positions int32 [axes x T] (None: each token's place in its sequence, on every axis).  Rows behind the last sequence are
+    most T; positions int32 [axes x T] (None: each token's place in its sequence, on every axis; the tables have to hold them).  Rows behind the last sequence are
     padding: their targets have to be outside the vocabulary, then they add nothing to any gradient.  The kernels read all of it on the
     device, so that a captured step takes any further batch."""
 
@@ -181,7 +181,7 @@ class PackedAttention:
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self.offsets = torch.zeros(max_sequences + 1, dtype=torch.int32, device=self.device)
         self.positions = torch.zeros(1 + max(self.pair_axis, default=0), T, dtype=torch.int32, device=self.device)
-        self.rows = None             # of the batch's sequences, from set_batch()
+        self.longest = None          # the most positions that set_batch() has counted in a sequence
 
     def set_batch(self, lengths, positions=None, stream=None) -> None:
         lengths = [int(n) for n in lengths]
@@ -191,20 +191,23 @@ class PackedAttention:
         for n in lengths:
             place[at[-1]:at[-1] + n] = torch.arange(n, dtype=torch.int32)
             at.append(at[-1] + n)
-        if positions is None:
+        counted = positions is None
+        if counted:
             positions = place.expand_as(self.positions)
         if tuple(positions.shape) != tuple(self.positions.shape):
             raise B.LomoError(f"positions {tuple(positions.shape)}, want {tuple(self.positions.shape)}")
-        self.rows = at[-1]
+        self.longest = max(lengths, default=0) if counted else 0
         with B.on_stream(stream):      # behind the steps that read the last batch's
             # the sequences that are not there are empty ones: the buffers, and what a captured step reads, stay the same
-            self.offsets.copy_(torch.tensor(at + [self.rows] * (self.offsets.numel() - len(at)), dtype=torch.int32))
+            self.offsets.copy_(torch.tensor(at + [at[-1]] * (self.offsets.numel() - len(at)), dtype=torch.int32))
             self.positions.copy_(positions)
 
     def forward(self, qkv, rope_cos, rope_sin, o, lse, stream=None) -> None:
         """qkv [T x qkv_width] as the projection leaves it: its q and k are turned in place."""
-        if self.rows is None:
+        if self.longest is None:
             raise B.LomoError("no batch: set_batch() comes before the step")
+        if self.longest > rope_cos.shape[0]:
+            raise B.LomoError(f"a sequence of {self.longest} tokens, rotary tables of {rope_cos.shape[0]} positions")
         B.lomo_rope_axes(qkv, qkv, rope_cos, rope_sin, self.positions, self.pair_axis, self.n_heads + self.n_kv_heads, self.head_dim,
                          stream=stream)
         B.lomo_window_attention_forward(qkv, o, lse, self.offsets, self.n_heads, self.n_kv_heads, self.window, self.sinks, stream)

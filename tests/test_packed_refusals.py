@@ -24,3 +24,19 @@ def test_clear_padding_arguments(lib):
         L.binding._check(call(24, 16, 4, 1, 8))
     with pytest.raises(L.LomoError):
         L.binding._check(call(16, 18, 4, 1, 8))
+
+
+def test_a_sequence_longer_than_the_rotary_tables(lib):
+    """Positions that the batch counts by itself have to be in the tables: pairs beyond them would stay unturned."""
+    import torch
+    from paper_2306_09782_amd.chain import PackedAttention
+    packed = PackedAttention("cpu", 100, 2, 1, 64)
+    qkv, o, lse = torch.zeros(100, 256, dtype=torch.float16), torch.zeros(100, 128, dtype=torch.float16), torch.zeros(100, 2)
+    cos, sin = torch.ones(40, 32), torch.zeros(40, 32)
+    packed.set_batch([30, 41, 2])
+    with pytest.raises(L.LomoError, match="41 tokens"):
+        packed.forward(qkv, cos, sin, o, lse)
+    for lengths, positions in (([40, 40], None), ([], None), ([100], torch.full((1, 100), 39, dtype=torch.int32)), ([100], torch.full((1, 100), -1, dtype=torch.int32))):
+        packed.set_batch(lengths, positions)
+        with pytest.raises(L.LomoError, match="x is on cpu"):      # taken, up to the device
+            packed.forward(qkv, cos, sin, o, lse)
