@@ -448,6 +448,14 @@ def _rows(t, T, width, name):
     return t.stride(0) if T > 1 else width
 
 
+def pair_axes(pair_axis) -> bytes:
+    """One byte for each entry of a sequence of whole numbers.  Arrays and tensors go entry by entry: bytes() would take their memory."""
+    try:
+        return bytes(pair_axis) if type(pair_axis) in (bytes, list, tuple) else bytes(int(a) for a in pair_axis)
+    except (TypeError, ValueError) as e:
+        raise LomoError(f"pair_axis: {e}") from None
+
+
 def lomo_rope_axes(x, y, rope_cos, rope_sin, positions, pair_axis, n_heads, head_dim, inverse=False, stream=None):
     """Rows of x and y may be longer than n_heads * head_dim and need not be adjacent; y may be x.  positions [axes x T];
     pair_axis: the axis of each of the head_dim / 2 pairs (bytes, or any sequence of int)."""
@@ -460,7 +468,7 @@ def lomo_rope_axes(x, y, rope_cos, rope_sin, positions, pair_axis, n_heads, head
     _expect(rope_cos, torch.float32, (P, head_dim // 2), device, "rope_cos")
     _expect(rope_sin, torch.float32, (P, head_dim // 2), device, "rope_sin")
     _expect(positions, torch.int32, (A, T), device, "positions")
-    axes = pair_axis if isinstance(pair_axis, bytes) else bytes(pair_axis)
+    axes = pair_axes(pair_axis)
     if len(axes) != head_dim // 2:
         raise LomoError(f"pair_axis has {len(axes)} entries, want {head_dim // 2}")
     _check(load_library().lomo_rope_axes(x.data_ptr(), ldx, y.data_ptr(), ldy, rope_cos.data_ptr(), rope_sin.data_ptr(), P,

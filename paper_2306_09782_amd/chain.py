@@ -173,7 +173,7 @@ class PackedAttention:
         self.device = torch.device(device)
         self.T, self.n_heads, self.n_kv_heads, self.head_dim = T, n_heads, n_kv_heads, head_dim
         self.window, self.sinks = (max(T, 1) if window is None else window), sinks
-        self.pair_axis = bytes(head_dim // 2) if pair_axis is None else bytes(pair_axis)
+        self.pair_axis = bytes(head_dim // 2) if pair_axis is None else B.pair_axes(pair_axis)
         self.qkv_width = (n_heads + 2 * n_kv_heads) * head_dim
         nbytes = B.lomo_window_attention_workspace_bytes(T, max_sequences, n_heads, n_kv_heads, head_dim, sinks)
         if T > 0 and max_sequences > 0 and nbytes == 0:

@@ -40,3 +40,18 @@ def test_a_sequence_longer_than_the_rotary_tables(lib):
         packed.set_batch(lengths, positions)
         with pytest.raises(L.LomoError, match="x is on cpu"):      # taken, up to the device
             packed.forward(qkv, cos, sin, o, lse)
+
+
+def test_axes_of_pairs_from_any_sequence():
+    """Lists, tuples, bytes, tensors and arrays of any whole type name the same axes; numbers that are no axes are refused."""
+    import numpy as np
+    import torch
+    from paper_2306_09782_amd.chain import PackedAttention
+    want = bytes([0, 1] * 16)
+    for given in (want, bytearray(want), list(want), tuple(want), np.array(list(want)), np.array(list(want), dtype=np.int32),
+                  np.array(list(want), dtype=np.uint8), torch.tensor(list(want))):
+        packed = PackedAttention("cpu", 8, 2, 1, 64, pair_axis=given)
+        assert packed.pair_axis == want and packed.positions.shape == (2, 8)
+    for bad in (32, [0, -1] * 16, [0, 256] * 16, ["a"] * 32, 1.5):
+        with pytest.raises(L.LomoError):
+            PackedAttention("cpu", 8, 2, 1, 64, pair_axis=bad)
