@@ -225,7 +225,7 @@ class PackedAttention:
 class LomoAttentionBlock:
     """Hand-on buffers of the attention block: do [T x H], [dq|dk|dv] [T x 3H], dxn [T x H], delta [T x heads].
     `saved`: o, xn, xhat [T x H], rstd [T] fp32, qkv [T x 3H] (rotated q and k, v), lse [T x heads] fp32.
-    With `packed` (PackedAttention) qkv and its gradient are packed.qkv_width wide."""
+    With `packed` (PackedAttention) qkv and its gradient are packed.qkv_width wide, and there is no delta."""
 
     def __init__(self, device, batch: int, seq: int, H: int, n_heads: int, state: StepState = None, slot0: int = 0,
                  share=None, packed: PackedAttention = None):
@@ -238,7 +238,8 @@ class LomoAttentionBlock:
         self.do = share.do if share is not None else torch.empty(T, H, **f16)
         self.dqkv = share.dqkv if share is not None else torch.empty(T, 3 * H if packed is None else packed.qkv_width, **f16)
         self.dxn = share.dxn if share is not None else torch.empty(T, H, **f16)
-        self.delta = share.delta if share is not None else torch.empty(T * n_heads, dtype=torch.float32, device=self.device)
+        if packed is None:           # its own workspace has that otherwise
+            self.delta = share.delta if share is not None else torch.empty(T * n_heads, dtype=torch.float32, device=self.device)
         self.state = state if state is not None else StepState(self.device, 3, T, H)
         self.slot0 = slot0
         self._lists = None

@@ -216,7 +216,7 @@ hipError_t launch_attention_backward(const uint16_t* qkv, const uint16_t* o, con
 // Operators for students and long packed sequences (lomo_rope_axes.hip, lomo_window_fwd.hip, lomo_window.hip, lomo_distill.hip).
 hipError_t launch_rope_axes(const uint16_t* x, int64_t ldx, uint16_t* y, int64_t ldy, const float* cosv, const float* sinv, int64_t P,
                             const int32_t* pos, const uint8_t* axis, int64_t T, int64_t heads, int64_t d, bool inverse, hipStream_t st);
-int64_t window_attention_threads(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks);      // the most workgroups of a launch
+int64_t window_attention_threads(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks);      // of the largest launch
 size_t window_attention_ws_bytes(int64_t T, int64_t B, int64_t h, int64_t g, int64_t d, int64_t sinks);
 hipError_t launch_window_attention_forward(const uint16_t* qkv, uint16_t* o, float* lse, const int32_t* off, int64_t T, int64_t B, int64_t h,
                                            int64_t g, int64_t d, int64_t window, int64_t sinks, hipStream_t st);

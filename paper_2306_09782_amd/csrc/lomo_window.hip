@@ -348,7 +348,7 @@ __global__ __launch_bounds__(256, 2) void window_attention_dq_kernel(win::BwdArg
             if (!active) continue;
 #pragma nounroll
             for (int h = 0; h < 2; ++h) {
-                if (seen(qw, k0 + 32 * h, window, sinks) == NONE) continue;
+                if (!seen(qw, k0 + 32 * h, window, sinks)) continue;
                 const TileRead<D> r1 = r0.at(32 * h * D);
                 uint32_t rows = __builtin_amdgcn_readfirstlane(bad[it & 1][2 * h] | bad[it & 1][2 * h + 1] << 16);
                 half8 f[2];

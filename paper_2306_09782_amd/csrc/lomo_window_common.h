@@ -90,12 +90,12 @@ __device__ __forceinline__ int swz(int r) {
     else return ((r & 2) << 1) | ((r >> 2) & 3);
 }
 
-// Load of [64 x D] tiles of rows `ld` elements apart, 64 of them less than 4 GiB.  Each of WAVES waves fetches WROWS neighbouring rows, RPI with an
+// Load of [64 x D] tiles of rows `ld` elements apart, 64 of them less than 4 GiB.  Each of four waves fetches WROWS neighbouring rows, RPI with an
 // instruction.  The instructions' swizzles differ from that of the first in two chunk bits; their offsets in memory and in LDS share the
 // immediate, so that one value of M0 serves them all.
-template <int D, int WAVES = 4>
+template <int D>
 struct TileLoad {
-    static constexpr int TROWS = BLK, WROWS = TROWS / WAVES, RPI = 512 / D, PER = WROWS / RPI;
+    static constexpr int TROWS = BLK, WROWS = TROWS / 4, RPI = 512 / D, PER = WROWS / RPI;
     uint32_t voff, ld2, step;
     __device__ __forceinline__ TileLoad(int64_t ld, int wave) {
         const int lane = threadIdx.x & 63, rr = lane / (D / 8), c = lane % (D / 8);
@@ -122,8 +122,6 @@ struct TileLoad {
                              "buffer_load_dwordx4 %2, %4, %6 offen offset:0x800 lds\n\t"
                              "buffer_load_dwordx4 %3, %4, %7 offen offset:0xc00 lds"
                              ::"v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(srd), "s"(step), "s"(2 * step), "s"(3 * step), "s"(lds) : "memory", "m0");
-            else if constexpr (PER == 1)
-                asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(v[0]), "s"(srd), "s"(lds) : "memory", "m0");
             else
                 asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\t"
                              "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
@@ -207,10 +205,10 @@ __device__ __forceinline__ void store_rows(const floatx16 (&acc)[N], uint16_t* r
 // A product over a block that a mask cuts has zeros for the hidden pairs, and 0 * inf is not 0: the moving operand of such tiles is made
 // finite in LDS first.  What sees the values all the same gets to know of them otherwise: their rows' lse and delta are not finite,
 // and the forward adds them.  Each wave looks through the rows that it fetched; returned is one bit for each row that held any (uniform).
-template <int D, int WAVES = 4>
+template <int D>
 __device__ __forceinline__ uint32_t make_finite(uint32_t tile, int wave) {
     typedef __attribute__((address_space(3))) u32x4* chunk_p;
-    using Load = TileLoad<D, WAVES>;
+    using Load = TileLoad<D>;
     constexpr int RPI = Load::RPI, LANES = 64 / RPI;      // of a row
     const int lane = threadIdx.x & 63;
     uint32_t rows = 0;
@@ -235,11 +233,9 @@ __device__ __forceinline__ uint32_t make_finite(uint32_t tile, int wave) {
 }
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
-// What a mask leaves of queries q0 .. q0 + 31 and keys k0 .. k0 + 31 (uniform in a wave).
-enum Seen { NONE, SOME, ALL };
-__device__ __forceinline__ Seen seen(int q0, int k0, int window, int sinks) {
-    if (k0 > q0 + 31 || (q0 - (k0 + 31) >= window && k0 >= sinks)) return NONE;
-    return k0 + 31 <= q0 && (q0 + 31 - k0 < window || k0 + 31 < sinks) ? ALL : SOME;
+// A mask leaves pairs of queries q0 .. q0 + 31 and keys k0 .. k0 + 31 (uniform in a wave).
+__device__ __forceinline__ bool seen(int q0, int k0, int window, int sinks) {
+    return k0 <= q0 + 31 && (q0 - (k0 + 31) < window || k0 < sinks);
 }
 
 }  // namespace win

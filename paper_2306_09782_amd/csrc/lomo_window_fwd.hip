@@ -165,10 +165,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void window_attention_forward
             if (lane == 0) bad[it & 1][wave] = mine;
             attn::meet();
             if (!active) continue;
-            bool none = true;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) none = none && seen(qw, k0 + 32 * h, window, sinks) == NONE;
-            if (none) continue;
+            if (!seen(qw, k0, window, sinks) && !seen(qw, k0 + 32, window, sinks)) continue;
             // of a distance that is negative or not below the window, but for the sinks
             auto hidden = [&](int key) { return (uint32_t)(query - key) >= (key < sinks ? 0x80000000u : (uint32_t)window); };
             floatx16 S[2];
