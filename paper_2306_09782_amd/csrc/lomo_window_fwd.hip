@@ -5,7 +5,7 @@
 //
 // One workgroup per (128 queries, head) walks the pairs of key and value tiles (64 keys) that the window of its queries reaches, the
 // tile of the sinks first where that is left of them; one pass with a running maximum and sum.  Workgroups are numbered so that the heads of a
-// group and neighbouring queries run on one XCD at a time.  Probabilities are rounded to fp16 relative to the running maximum, as the matrix
+// group and neighbouring queries run on one XCD at a time.  Probabilities are rounded to fp16 relative to a running reference, as the matrix
 // cores take them; sums and accumulators are fp32; o is rounded once.  Deterministic, and independent of what else is in the batch.
 //
 // Tiles that every query of the workgroup sees whole have a loop of their own, without masks.  A key that the mask hides from a query adds nothing
@@ -98,10 +98,11 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void window_attention_forward
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) S = __builtin_amdgcn_mfma_f32_32x32x16_f16(r0.rows(32 * h * D, ks), fq[ks], S, 0, 0, 0);
     };
-    // From scores to probabilities relative to the running maximum, in fp16.  The maximum moves only where it has grown by more than
-    // SLACK: probabilities stay below 2^SLACK, and most tiles leave sum and output as they are.  Each query moves by its own scores alone,
-    // so that no bit of its result depends on what its neighbours see.
-    constexpr float SLACK = 8.f;
+    // From scores to probabilities relative to a running reference, in fp16.  The reference begins 2^LIFT below the maximum, so that
+    // probabilities down to 2^-21 of the largest are normal numbers of fp16, and moves only where the maximum has grown by more than 2^SLACK:
+    // probabilities stay below 2^(LIFT + SLACK), and most tiles leave sum and output as they are.  Each query moves by its own scores alone,
+    // so that no bit of its result depends on what its neighbours see.  SLACK 0 / 2 / 4 / 8, us: long 1090 / 1058 / 1045 / 1025, odd 99 / 96.5 / 96 / 93.5.
+    constexpr float LIFT = 7.f, SLACK = 8.f;
     auto probabilities = [&](const floatx16 (&S)[2], uint32_t (&pk)[2][8]) {
         float top = -INFINITY;
 #pragma unroll
@@ -110,9 +111,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void window_attention_forward
             for (int e = 0; e < 16; ++e) top = fmaxf(top, S[h][e]);
         const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * C2;
-        if (__any(top > m_run + SLACK)) {
-            const bool grown = top > m_run + SLACK;
-            const float m_new = grown ? top : m_run, alpha = grown ? __builtin_amdgcn_exp2f(m_run - top) : 1.f;
+        if (__any(top > m_run + (LIFT + SLACK))) {
+            const bool grown = top > m_run + (LIFT + SLACK);
+            const float m_new = grown ? top - LIFT : m_run, alpha = grown ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
 #pragma unroll
             for (int i = 0; i < NC; ++i)
 #pragma unroll
