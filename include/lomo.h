@@ -385,7 +385,7 @@ lomo_status lomo_cross_entropy_mean(const lomo_half* logits, const int32_t* targ
 
 /* ---------------------------------------------------------------- students and long packed sequences
  * Steps that take the place of lomo_rope_forward, lomo_attention_forward / _backward and lomo_cross_entropy(_mean) where a
- * model is fine-tuned on sequences of any length packed into one batch, with pictures or video among the tokens, with heads that share
+ * model is fine-tuned on sequences of any length packed into one batch, with positions on several axes, with heads that share
  * keys and values, with attention that reaches a limited distance, or from a teacher.  Same storage convention (fp16 tensors, fp32
  * arithmetic, one rounding per stored element). */
 

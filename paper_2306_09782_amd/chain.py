@@ -164,9 +164,10 @@ class PackedAttention:
     [positions x head_dim / 2].  window=None: no limit.  pair_axis: the axis of each of the head_dim / 2 pairs (None: one axis).
 
     set_batch(lengths, positions) before a step, on the step's stream: lengths on the host, at most max_sequences of them, their sum at
-    most T; positions int32 [axes x T] (None: each token's place in its sequence, on every axis; the tables have to hold them).  Rows behind the last sequence are
-    padding: their targets have to be outside the vocabulary, then they add nothing to any gradient.  The kernels read all of it on the
-    device, so that a captured step takes any further batch."""
+    most T; positions int32 [axes x T] (None: each token's place in its sequence, on every axis; the tables have to hold them).  Rows
+    behind the last sequence are padding: their targets have to be outside the vocabulary, then they add nothing to any gradient.  The
+    kernels read all of it on the device, so that a captured step takes any further batch.  Steps that overlap in time, eager or replayed,
+    need an object each: it holds the backward pass's workspace."""
 
     def __init__(self, device, T: int, n_heads: int, n_kv_heads: int, head_dim: int, window: int = None, sinks: int = 0,
                  max_sequences: int = 64, pair_axis=None):
@@ -211,7 +212,7 @@ class PackedAttention:
         B.lomo_rope_axes(qkv, qkv, rope_cos, rope_sin, self.positions, self.pair_axis, self.n_heads + self.n_kv_heads, self.head_dim,
                          stream=stream)
         B.lomo_window_attention_forward(qkv, o, lse, self.offsets, self.n_heads, self.n_kv_heads, self.window, self.sinks, stream)
-        B.lomo_clear_padding(o, self.offsets, stream)       # the attention leaves rows of no sequence as they are; the products that follow take them all
+        B.lomo_clear_padding(o, self.offsets, stream)       # left as they were; the products that follow take all rows
 
     def backward(self, qkv, o, dO, lse, rope_cos, rope_sin, dqkv, stream=None) -> None:
         """dqkv: the gradient of the projection's output."""

@@ -16,13 +16,14 @@
 // gradients of any size do.  dq, dk, dv are rounded once.  Tiles that a mask cuts are
 // made finite first, so that a pair which the mask hides adds nothing; a query that sees a key which is not finite has NaN in its gradient.
 //
-// Measured, us: 16384 tokens, 32 / 8 heads of 128, window 2048, 4 sinks 2190 (dq 800, dk and dv 1390; 588 TFLOP/s of the five products, 820 of
-// the seven executed); 4096 rows of seven sequences, window 1024 189; four short sequences 25.  Power bounds the long ones: the clock falls below
-// 2.0 GHz with the matrix cores busy for half (dq) and a third (dk, dv) of its cycles, and what takes stalls away changes nothing: three pairs of
-// tiles in flight, one barrier a tile with the partner's half multiplied beside the next scores, no exponentials (1 %), no meeting of partners
-// (1 %).  Fewer bytes do: without tile loads 18 % of dk and dv less.  A packed batch is bound by its longest walk: the two teams of a workgroup
-// took it from 206 to 189 (short 29 -> 25; 16384 tokens, where there are walks enough, 2090 -> 2190).  Both teams on 128 keys and the same tiles:
-// 2065, but 222 and 30; by the size of a call it would make a sequence's bits depend on its batch.
+// Measured, us: 16384 tokens, 32 / 8 heads of 128, window 2048, 4 sinks 2130 (dq 800, dk and dv 1330; 605 TFLOP/s of the five products, 845 of
+// the seven executed); 4096 rows of seven sequences, window 1024 192 to 198; 8192 tokens, 32 / 8 heads of 64, window 2048 635 (473 TFLOP/s); four short
+// sequences 25.  Power bounds dq of the long ones: the clock falls to 1.8 GHz with the matrix cores busy for half of its cycles.  dk and dv have them busy for
+// 36 % at 1.94 GHz and are bound by the bytes of their moving tiles: without tile loads they take 18 % less, and what takes stalls away changes
+// nothing (three pairs of tiles in flight, one barrier a tile with the partner's half multiplied beside the next scores, no exponentials 1 %, no
+// meeting of partners 1 %).  A packed batch is bound by its longest walk: two teams in a workgroup took it from 206 to 189 (short 29 -> 25; 16384 tokens,
+// where there are walks enough, 2090 -> 2190).  Both teams on 128 keys and the same tiles: 2065 then, but 222 and 30, so the choice would be the
+// sequence's: by its own length, window and group, since by the size of the call its bits would depend on its batch.
 #include "lomo_window_common.h"
 
 #include <algorithm>
@@ -32,7 +33,7 @@ namespace lomo {
 
 namespace win {
 
-constexpr int FAR_ROWS = 512;
+constexpr int FAR_ROWS = 512;      // 256 / 512 / 1024, us: long 2185 / 2160 / 2215, packed 194.5 / 192 / 194
 constexpr float P_SCALE = 32768.f, P_LOG2 = 15.f;
 template <int D>
 constexpr float DS_SCALE = SCALE<D> / P_SCALE;      // of dP - delta where it meets P times P_SCALE

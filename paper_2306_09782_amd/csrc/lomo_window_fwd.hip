@@ -6,14 +6,15 @@
 // One workgroup per (128 queries, head) walks the pairs of key and value tiles (64 keys) that the window of its queries reaches, the
 // tile of the sinks first where that is left of them; one pass with a running maximum and sum.  Workgroups are numbered so that the heads of a
 // group and neighbouring queries run on one XCD at a time.  Probabilities are rounded to fp16 relative to a running reference, as the matrix
-// cores take them; sums and accumulators are fp32; o is rounded once.  Deterministic, and independent of what else is in the batch.
+// cores take them (o is off by 2.5e-4 of its norm, 2.0e-4 of which is its own rounding; with what the rounding of P leaves in a further product it would be
+// 2.0e-4, at 1345 us instead of 1000, packed 68 instead of 54); sums and accumulators are fp32; o is rounded once.  Deterministic, and independent of what else is in the batch.
 //
 // Tiles that every query of the workgroup sees whole have a loop of their own, without masks.  A key that the mask hides from a query adds nothing
 // to it, whatever its v holds: inf and NaN are taken out of the tiles that a mask cuts, and added to the queries that do see them.
 //
-// Measured, us: 16384 tokens, 32 / 8 heads of 128, window 4096, 4 sinks 1025 (940 TFLOP/s of the visible pairs); 8192 tokens, 32 heads, no window 575
-// (955 TFLOP/s); 4096 rows of seven sequences, window 1024 53; 8192 tokens, 32 / 8 heads of 64, window 2048 168 (716 TFLOP/s); four short sequences 6.8,
-// the time of a launch.  Power is what bounds the long ones: the clock is at 1.5 to 1.9 GHz with the matrix cores busy for 47 to 52 % of its cycles and the vector
+// Measured, us: 16384 tokens, 32 / 8 heads of 128, window 4096, 4 sinks 990 to 1025 (940 TFLOP/s of the visible pairs); 8192 tokens, no window, 32 / 8 heads
+// of 128 570 (965 TFLOP/s); 4096 rows of seven sequences, window 1024 53; 8192 tokens, 32 / 8 heads of 64, window 2048 168 (716 TFLOP/s); four short
+// sequences 6.8, the time of a launch.  Power is what bounds the long ones: the clock is at 1.5 to 1.9 GHz with the matrix cores busy for 47 to 52 % of its cycles and the vector
 // units for 55 %.  Slower or no faster: the next tile's scores between the probabilities (1300), two waves of a SIMD held half a step apart by
 // barriers (1000, and short sequences 30 % slower), tiles of 32 keys with three waves a SIMD (1010, odd lengths 12 % slower).
 #include "lomo_window_common.h"
